@@ -398,6 +398,152 @@ int s2moe_adaptive_expand(int32_t n_cand, int32_t n_layers, int32_t n_experts, c
                           float t_exp, int32_t *admitted, int32_t *order, int32_t *n_admitted,
                           uint64_t *union_out, void *cuda_stream);
 
+/*
+ * ---- Attention around the layer, and the key/value cache under it --------------------------
+ *
+ * A target model runs attention between its MoE layers.  Draft and target share one cache, the
+ * drafted tokens' keys and values are temporary and only accepted tokens are committed (Sec. 4.3,
+ * "Context-aligned self-speculation"): a prompt is attended to as a whole (s2moe_prompt_attention)
+ * and written (s2moe_kv_write); a verification step writes its drafted tokens behind the context,
+ * attends with the tree (s2moe_tree_attention) and commits the accepted path (s2moe_kv_commit).
+ * s2moe_pages_* keeps book of the pages on the host, s2moe_kv_copy_pages does the copies that it names.
+ *
+ * None of these calls uses a context or allocates device memory; all but s2moe_attention_status and
+ * s2moe_pages_* are asynchronous on the given stream, run on the current device and may be captured.
+ * They read lengths and page numbers on the device, so a captured call follows them.
+ * Types: S2MOE_F32 and S2MOE_BF16 (all operands of a call alike); scores, softmax statistics and sums in
+ * binary32.  With S2MOE_BF16 the weights of a softmax are rounded to bfloat16 before the product with the values.
+ */
+
+/* A paged cache of n_layers layers.  k, v: dev, 16-byte aligned, [n_layers][n_pages][n_kv_heads][page_size][head_dim].
+ * head_dim 64 or 128; page_size 16, 32, 64 or 128; n_pages * n_kv_heads * page_size below 2^31.
+ * Position p of sequence s lies in page page_table[s][p / page_size] at place p % page_size. */
+typedef struct {
+    void *k;
+    void *v;
+    int32_t dtype;         /* S2MOE_F32 or S2MOE_BF16 */
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t n_kv_heads;
+    int32_t page_size;
+    int32_t head_dim;
+} s2moe_kv_cache;
+
+#define S2MOE_ATTN_MAX_GROUP 64      /* query heads per key/value head                        */
+#define S2MOE_TREE_MAX_NODES 64      /* nodes of a tree that has parents (chains: any number)   */
+#define S2MOE_COMMIT_MAX_PATH 64     /* accepted tokens of one commit                         */
+
+/*
+ * Causal attention over whole prompts, packed one behind the other:
+ *   out[t][h] = sum_{j <= t} softmax_j(scale * q[t][h] . k[j][h / (n_heads / n_kv_heads)]) v[j][...]
+ * over the tokens j of t's own sequence.
+ *   q          dev [n_tokens][n_heads][head_dim], q_stride elements from token to token (so that q, k and v can be
+ *              parts of one projection's output); 16-byte aligned, strides multiples of 16 bytes
+ *   k, v       dev [n_tokens][n_kv_heads][head_dim] with their strides
+ *   seq_start  dev [n_seq + 1] int32: sequence s has tokens seq_start[s] .. seq_start[s+1]-1; tokens of no
+ *              sequence are left out and their rows of out stay as they are
+ *   out        dev [n_tokens][n_heads][head_dim], 16-byte aligned, must not overlap the inputs
+ * A key that a row does not see has no part in it, whatever it holds (infinities and NaN too).
+ * Errors: EINVAL (null, alignment, heads, head_dim, scale negative or not finite), ERANGE (n_tokens * n_heads
+ * beyond 2^31 - 1), ECUDA.
+ */
+int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads,
+                           int32_t head_dim, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           const void *v, int64_t v_stride, const int32_t *seq_start, float scale, void *out,
+                           void *cuda_stream);
+
+/*
+ * Attention of trees of drafted tokens over the cache.  Sequence s has context[s] committed positions, behind them the
+ * nodes of its tree (node i at position context[s] + i, already written).  A token sees the committed positions,
+ * its own node and the node's ancestors.
+ *   q            dev [n_tokens][n_heads][head_dim], q_stride elements from token to token
+ *   page_table   dev [n_seq][table_width] int32; positions beyond the table and pages outside the cache are
+ *                not there for any row (a row that sees nothing becomes zero)
+ *   context      dev [n_seq] int32
+ *   seq_start    dev [n_seq + 1] int32: tokens of every sequence, as in s2moe_prompt_attention
+ *   n_nodes, node_start, parent
+ *                node_start dev [n_seq + 1] int32, or NULL (then n_nodes must be n_tokens): the tokens are the nodes.
+ *                With it a tree may have more nodes than tokens; the tokens are its last ones (a draft that
+ *                adds a level to a tree whose other nodes are in the cache).  parent dev [n_nodes] int32: index of a
+ *                node's parent within its tree, -1 for none (any value that does not come before the node counts
+ *                as none); or NULL: chains, every node sees all before it.
+ *                A sequence with more tokens than nodes, or with parents and more than S2MOE_TREE_MAX_NODES
+ *                nodes, gets NaN.
+ *   out          dev [n_tokens][n_heads][head_dim], must not overlap the inputs
+ *   workspace    dev, 16-byte aligned, at least what s2moe_tree_attention_workspace says; contents do not matter
+ *                before or after.  Calls that may run at the same time need one each, captured graphs too.
+ * One token per sequence is plain decoding.  Results depend on the arguments alone, not on timing.
+ * Errors: EINVAL, ERANGE (layer, n_tokens * n_heads or table_width * page_size beyond 2^31), ECUDA.
+ */
+int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, int32_t n_heads,
+                         const void *q, int64_t q_stride, const int32_t *page_table, int32_t table_width,
+                         const int32_t *context, const int32_t *seq_start, int32_t n_nodes, const int32_t *node_start,
+                         const int32_t *parent, float scale, void *out, void *workspace, int64_t workspace_bytes,
+                         void *cuda_stream);
+int s2moe_tree_attention_workspace(const s2moe_kv_cache *cache, int32_t n_seq, int32_t n_tokens, int32_t n_heads,
+                                   int32_t table_width, int64_t *bytes);
+
+/* Synchronises the device, stores the attention kernels' status word (0 = no bounded wait gave up since the last
+ * look; otherwise results since then are void) in *host_out and clears it.  ETIMEOUT if it was non-zero. */
+int s2moe_attention_status(int32_t *host_out);
+
+/*
+ * Keys and values of new tokens into one layer of the cache: token i of sequence s goes to position first[s] + i.
+ *   k, v       dev [n_tokens][n_kv_heads][head_dim], strides in elements; 16-byte aligned, strides multiples of 16 bytes
+ *   first      dev [n_seq] int32
+ *   seq_start  dev [n_seq + 1] int32
+ * Tokens of no sequence, positions outside the table and pages outside the cache are left out.
+ */
+int s2moe_kv_write(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, const void *k,
+                   int64_t k_stride, const void *v, int64_t v_stride, const int32_t *page_table, int32_t table_width,
+                   const int32_t *first, const int32_t *seq_start, void *cuda_stream);
+
+/*
+ * Commit accepted paths in all layers: the key and value at position context[s] + path[s][i] move to position
+ * context[s] + i, for i < n_path[s] (clamped to 0..max_path), as if all were read before any is written: a path
+ * may be in any order and name a node twice.
+ *   path         dev [n_seq][max_path] int32, 1 <= max_path <= S2MOE_COMMIT_MAX_PATH; negative nodes, positions outside
+ *                the table and pages outside the cache are left out
+ *   new_context  dev [n_seq] int32, written: context[s] + n_path[s]; must not overlap context
+ */
+int s2moe_kv_commit(const s2moe_kv_cache *cache, int32_t n_seq, const int32_t *page_table, int32_t table_width,
+                    const int32_t *context, const int32_t *path, int32_t max_path, const int32_t *n_path,
+                    int32_t *new_context, void *cuda_stream);
+
+/*
+ * Copy whole pages in all layers.  pairs: HOST [n_pairs][2] int32 {from, to}, read before the call returns.
+ * Errors: ERANGE (page outside the cache), EINVAL (a page is written twice, or both written and read), ENOMEM.
+ */
+int s2moe_kv_copy_pages(const s2moe_kv_cache *cache, int32_t n_pairs, const int32_t *pairs, void *cuda_stream);
+
+/*
+ * Who owns which page: a host-only object (no CUDA call).  A sequence is a list of pages; a fork shares its parent's.
+ *   open      a new, empty sequence (numbers of closed ones are given again)
+ *   fork      a new sequence with the same pages
+ *   reserve   pages for positions from .. to-1 that the sequence alone owns, and for all before them: missing ones are
+ *             taken, lowest number first, a shared one is replaced; pairs_out gets the {from, to} copies that
+ *             s2moe_kv_copy_pages has to make before the positions are written.  ENOMEM: not enough free pages
+ *             (nothing changed); ERANGE: unknown sequence, or more than max_pairs pairs (*n_pairs_out says how many,
+ *             nothing changed)
+ *   truncate  gives back the pages behind the first `length` positions
+ *   close     gives back all pages and the number
+ *   list      the pages of a sequence (a row of the page table); ERANGE when there are more than max_pages
+ *   compact   moves the pages in use to the lowest numbers; pairs_out gets the copies.  ERANGE: more than max_pairs
+ * One thread at a time per object.
+ */
+typedef struct s2moe_pages s2moe_pages;
+int s2moe_pages_create(int32_t n_pages, int32_t page_size, s2moe_pages **out);
+int s2moe_pages_destroy(s2moe_pages *pages);
+int s2moe_pages_open(s2moe_pages *pages, int32_t *seq_out);
+int s2moe_pages_fork(s2moe_pages *pages, int32_t seq, int32_t *seq_out);
+int s2moe_pages_reserve(s2moe_pages *pages, int32_t seq, int64_t from, int64_t to, int32_t max_pairs, int32_t *pairs_out,
+                        int32_t *n_pairs_out);
+int s2moe_pages_truncate(s2moe_pages *pages, int32_t seq, int64_t length);
+int s2moe_pages_close(s2moe_pages *pages, int32_t seq);
+int s2moe_pages_list(const s2moe_pages *pages, int32_t seq, int32_t max_pages, int32_t *pages_out, int32_t *n_pages_out);
+int s2moe_pages_free_count(const s2moe_pages *pages, int32_t *out);
+int s2moe_pages_compact(s2moe_pages *pages, int32_t max_pairs, int32_t *pairs_out, int32_t *n_pairs_out);
+
 #ifdef __cplusplus
 }
 #endif

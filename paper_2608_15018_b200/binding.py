@@ -27,7 +27,10 @@ EXPORTS = ("s2moe_create", "s2moe_verify_layer", "s2moe_verify_stack", "s2moe_ve
            "s2moe_profile_begin", "s2moe_profile_end", "s2moe_kernel_class_name", "s2moe_kernel_plan",
            "s2moe_route_noalloc", "s2moe_route_noalloc_status", "s2moe_expert_masks", "s2moe_adaptive_expand", "s2moe_create_offloaded",
            "s2moe_residency_stats", "s2moe_residency_uses", "s2moe_cache_create", "s2moe_cache_access",
-           "s2moe_cache_destroy")
+           "s2moe_cache_destroy", "s2moe_prompt_attention", "s2moe_tree_attention", "s2moe_tree_attention_workspace",
+           "s2moe_attention_status", "s2moe_kv_write", "s2moe_kv_commit", "s2moe_kv_copy_pages", "s2moe_pages_create",
+           "s2moe_pages_destroy", "s2moe_pages_open", "s2moe_pages_fork", "s2moe_pages_reserve", "s2moe_pages_truncate",
+           "s2moe_pages_close", "s2moe_pages_list", "s2moe_pages_free_count", "s2moe_pages_compact")
 OFFLOADED_FIELDS = ("w_gate", "w_up", "w_down", "s_gate", "s_up", "s_down")   # host tensors of an offloaded context
 NOALLOC_MAX_TOKENS, NOALLOC_MAX_EXPERTS = 64, 128
 KERNEL_CLASSES = 7
@@ -39,6 +42,12 @@ class LayerWeightsC(ctypes.Structure):
 
 class ResidencyC(ctypes.Structure):
     _fields_ = [("n_slots", ctypes.c_int32), ("n_pinned", ctypes.c_int32), ("pinned", ctypes.c_void_p)]
+
+
+class KVCacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("n_layers", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
 
 
 class ConfigC(ctypes.Structure):
@@ -129,6 +138,18 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.s2moe_cache_access.restype = ctypes.c_int
     lib.s2moe_cache_destroy.argtypes = [vp]
     lib.s2moe_cache_destroy.restype = ctypes.c_int
+    i64, f32, kv, pi32 = ctypes.c_int64, ctypes.c_float, ctypes.POINTER(KVCacheC), ctypes.POINTER(i32)
+    for name, args in dict(
+            prompt_attention=[i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, f32, vp, vp],
+            tree_attention=[kv, i32, i32, i32, i32, vp, i64, vp, i32, vp, vp, i32, vp, vp, f32, vp, vp, i64, vp],
+            tree_attention_workspace=[kv, i32, i32, i32, i32, ctypes.POINTER(i64)], attention_status=[pi32],
+            kv_write=[kv, i32, i32, i32, vp, i64, vp, i64, vp, i32, vp, vp, vp],
+            kv_commit=[kv, i32, vp, i32, vp, vp, i32, vp, vp, vp], kv_copy_pages=[kv, i32, vp, vp],
+            pages_create=[i32, i32, ctypes.POINTER(vp)], pages_destroy=[vp], pages_open=[vp, pi32], pages_fork=[vp, i32, pi32],
+            pages_reserve=[vp, i32, i64, i64, i32, vp, pi32], pages_truncate=[vp, i32, i64], pages_close=[vp, i32],
+            pages_list=[vp, i32, i32, vp, pi32], pages_free_count=[vp, pi32], pages_compact=[vp, i32, vp, pi32]).items():
+        getattr(lib, "s2moe_" + name).argtypes = args
+        getattr(lib, "s2moe_" + name).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -480,6 +501,271 @@ class ExpertCache:
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:
             self._lib.s2moe_cache_destroy(self._h)
+            self._h = ctypes.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---- attention and its key/value cache ------------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _on_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor on the current device, the one the kernels are launched on."""
+    if device.type != "cuda" or device.index != _device():
+        raise ValueError(f"tensors on {device}, but the current device is cuda:{_device()}")
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+
+
+def _int32(name: str, t: Optional[torch.Tensor], *shape: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous int32 {list(shape)} expected, got {t.dtype} {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _rows(name: str, t: torch.Tensor, heads: int, dim: int, dtype: torch.dtype) -> Tuple[int, int]:
+    """Address and token stride of [tokens][heads][dim] whose tokens may lie apart."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype:
+        raise ValueError(f"{name}: {dtype} [tokens][{heads}][{dim}] expected, got {t.dtype} {list(t.shape)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (t.shape[0] > 1 and t.stride(0) < heads * dim):
+        raise ValueError(f"{name}: the heads of a token must lie side by side, strides are {t.stride()}")
+    stride = t.stride(0) if t.shape[0] > 1 else heads * dim
+    if t.data_ptr() % 16 or stride * t.element_size() % 16:
+        raise ValueError(f"{name}: tokens must start on 16-byte boundaries")
+    return t.data_ptr(), stride
+
+
+def _output(out: Optional[torch.Tensor], like: torch.Tensor) -> torch.Tensor:
+    if out is None:
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    if out.dtype != like.dtype or out.shape != like.shape or not out.is_contiguous() or out.device != like.device:
+        raise ValueError(f"out: contiguous {like.dtype} {list(like.shape)} on {like.device} expected")
+    return out
+
+
+def _seqs(seq_start: torch.Tensor) -> int:
+    if seq_start.dim() != 1 or seq_start.shape[0] < 1:
+        raise ValueError("seq_start: [n_seq + 1] expected")
+    return seq_start.shape[0] - 1
+
+
+class KVCache:
+    """A paged key/value cache: ``k`` and ``v`` are the caller's [n_layers][n_pages][n_kv_heads][page_size][head_dim]
+    tensors (float32 or bfloat16, contiguous).  ``KVCache.empty`` makes them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.device != v.device or k.dtype not in _DTYPES:
+            raise ValueError("k and v: float32 or bfloat16 [n_layers][n_pages][n_kv_heads][page_size][head_dim], alike")
+        self.k, self.v = k, v
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype, self.device = k.dtype, k.device
+        self._c = KVCacheC(_dptr(k), _dptr(v), _DTYPES[k.dtype], *k.shape)
+        self._ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def empty(n_layers: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
+              device: Optional[torch.device] = None) -> "KVCache":
+        shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+        device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        return KVCache(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_start: torch.Tensor, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Causal attention over packed prompts through ``s2moe_prompt_attention``.  ``q`` [tokens][heads][dim], ``k`` and
+    ``v`` [tokens][kv heads][dim] (parts of one projection's output are fine), ``seq_start`` int32 [n_seq + 1].
+    Tokens of no sequence keep their rows of ``out``."""
+    lib = load_library()
+    n_seq = _seqs(seq_start)
+    if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or v.shape != k.shape or q.dtype not in _DTYPES:
+        raise ValueError("q: float32 or bfloat16 [tokens][heads][dim]; k, v: [tokens][kv heads][dim]")
+    n, heads, dim = q.shape
+    _on_device(q.device, k=k, v=v, seq_start=seq_start)
+    qp, qs = _rows("q", q, heads, dim, q.dtype)
+    kp, ks = _rows("k", k, k.shape[1], dim, q.dtype)
+    vp, vs = _rows("v", v, k.shape[1], dim, q.dtype)
+    starts = _int32("seq_start", seq_start, n_seq + 1)
+    out = _output(out, q)
+    rc = lib.s2moe_prompt_attention(_DTYPES[q.dtype], n_seq, n, heads, k.shape[1], dim, qp, qs, kp, ks, vp, vs, starts,
+                                    dim ** -0.5 if scale is None else float(scale), out.data_ptr(), _stream_handle(stream))
+    if rc != OK:
+        raise S2MoEError(rc, "s2moe_prompt_attention")
+    return out
+
+
+def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, page_table: torch.Tensor, context: torch.Tensor,
+                   seq_start: torch.Tensor, parent: Optional[torch.Tensor] = None, node_start: Optional[torch.Tensor] = None,
+                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention of drafted tokens over the cache through ``s2moe_tree_attention``.  ``q`` [tokens][heads][dim];
+    ``page_table`` int32 [n_seq][width]; ``context`` int32 [n_seq]; ``parent`` int32 [nodes] (index within the tree, -1:
+    none) or None for chains; ``node_start`` int32 [n_seq + 1] where the trees have more nodes than tokens.
+    The workspace is taken from torch's allocator per call, on the stream of the call."""
+    lib = load_library()
+    n_seq = _seqs(seq_start)
+    if q.dim() != 3 or page_table.dim() != 2:
+        raise ValueError("q: [tokens][heads][dim], page_table: [n_seq][width]")
+    n, heads, dim = q.shape
+    width = page_table.shape[1]
+    _on_device(q.device, cache=cache.k, page_table=page_table, context=context, seq_start=seq_start, parent=parent,
+               node_start=node_start)
+    if dim != cache.head_dim:
+        raise ValueError(f"q has heads of {dim}, the cache of {cache.head_dim}")
+    qp, qs = _rows("q", q, heads, dim, cache.dtype)
+    n_nodes = n if node_start is None or parent is None else parent.shape[0]
+    if node_start is not None and parent is None:
+        raise ValueError("node_start needs parent")
+    table, ctx = _int32("page_table", page_table, n_seq, width), _int32("context", context, n_seq)
+    starts, nodes = _int32("seq_start", seq_start, n_seq + 1), _int32("node_start", node_start, n_seq + 1)
+    par = _int32("parent", parent, n_nodes)
+    out = _output(out, q)
+    need = ctypes.c_int64(0)
+    rc = lib.s2moe_tree_attention_workspace(cache._ref, n_seq, n, heads, width, ctypes.byref(need))
+    if rc == OK:
+        ws = None
+        if need.value:
+            if stream is None:
+                ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+            else:
+                with torch.cuda.stream(stream):
+                    ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        rc = lib.s2moe_tree_attention(cache._ref, int(layer), n_seq, n, heads, qp, qs, table, width, ctx, starts, n_nodes, nodes,
+                                      par, dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
+                                      None if ws is None else ws.data_ptr(), need.value, _stream_handle(stream))
+    if rc != OK:
+        raise S2MoEError(rc, "s2moe_tree_attention")
+    return out
+
+
+def attention_status() -> int:
+    """Status word of the attention kernels on the current device (0: no bounded wait gave up since the last look).
+    Synchronises the device."""
+    out = ctypes.c_int32(0)
+    rc = load_library().s2moe_attention_status(ctypes.byref(out))
+    if rc not in (OK, ETIMEOUT):
+        raise S2MoEError(rc, "s2moe_attention_status")
+    return int(out.value)
+
+
+def kv_write(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, first: torch.Tensor,
+             seq_start: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Keys and values [tokens][kv heads][dim] into one layer through ``s2moe_kv_write``: token i of sequence s goes to
+    position ``first[s]`` + i."""
+    lib = load_library()
+    n_seq = _seqs(seq_start)
+    if page_table.dim() != 2 or k.shape != v.shape:
+        raise ValueError("page_table: [n_seq][width]; k and v alike")
+    width = page_table.shape[1]
+    _on_device(cache.device, k=k, v=v, page_table=page_table, first=first, seq_start=seq_start)
+    kp, ks = _rows("k", k, cache.n_kv_heads, cache.head_dim, cache.dtype)
+    vp, vs = _rows("v", v, cache.n_kv_heads, cache.head_dim, cache.dtype)
+    rc = lib.s2moe_kv_write(cache._ref, int(layer), n_seq, k.shape[0], kp, ks, vp, vs, _int32("page_table", page_table, n_seq, width),
+                            width, _int32("first", first, n_seq), _int32("seq_start", seq_start, n_seq + 1),
+                            _stream_handle(stream))
+    if rc != OK:
+        raise S2MoEError(rc, "s2moe_kv_write")
+
+
+def kv_commit(cache: KVCache, page_table: torch.Tensor, context: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
+              out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Commit accepted paths in all layers through ``s2moe_kv_commit``; ``path`` int32 [n_seq][most], ``n_path`` int32
+    [n_seq].  Returns the new contexts (``out``, which must not be ``context``)."""
+    lib = load_library()
+    if page_table.dim() != 2 or path.dim() != 2:
+        raise ValueError("page_table: [n_seq][width], path: [n_seq][most]")
+    n_seq, width = page_table.shape
+    _on_device(cache.device, page_table=page_table, context=context, path=path, n_path=n_path)
+    out = _output(out, context)
+    rc = lib.s2moe_kv_commit(cache._ref, n_seq, _int32("page_table", page_table, n_seq, width), width,
+                             _int32("context", context, n_seq), _int32("path", path, n_seq, path.shape[1]), path.shape[1],
+                             _int32("n_path", n_path, n_seq), out.data_ptr(), _stream_handle(stream))
+    if rc != OK:
+        raise S2MoEError(rc, "s2moe_kv_commit")
+    return out
+
+
+def kv_copy_pages(cache: KVCache, pairs: Sequence[Tuple[int, int]], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Copy whole pages (from, to) in all layers through ``s2moe_kv_copy_pages``; ``pairs`` is host data, for example what
+    ``PagePool.reserve`` or ``PagePool.compact`` returned."""
+    lib = load_library()
+    _on_device(cache.device)
+    flat = [int(x) for pair in pairs for x in pair]
+    if len(flat) != 2 * len(pairs):
+        raise ValueError("pairs: (from, to)")
+    arr = (ctypes.c_int32 * max(1, len(flat)))(*flat)
+    rc = lib.s2moe_kv_copy_pages(cache._ref, len(pairs), ctypes.cast(arr, ctypes.c_void_p), _stream_handle(stream))
+    if rc != OK:
+        raise S2MoEError(rc, "s2moe_kv_copy_pages")
+
+
+class PagePool:
+    """Who owns which page of a cache, host only (``s2moe_pages_*``)."""
+
+    def __init__(self, n_pages: int, page_size: int):
+        self._lib = load_library()
+        self._h = ctypes.c_void_p(None)
+        self.n_pages, self.page_size = int(n_pages), int(page_size)
+        self._call("create", self.n_pages, self.page_size, ctypes.byref(self._h))
+
+    def _call(self, name: str, *args) -> None:
+        rc = getattr(self._lib, "s2moe_pages_" + name)(*args)
+        if rc != OK:
+            raise S2MoEError(rc, "s2moe_pages_" + name)
+
+    def _number(self, name: str, *args) -> int:
+        out = ctypes.c_int32(0)
+        self._call(name, self._h, *args, ctypes.byref(out))
+        return out.value
+
+    def _pairs(self, name: str, *args) -> List[Tuple[int, int]]:
+        arr, n = (ctypes.c_int32 * (2 * self.n_pages))(), ctypes.c_int32(0)
+        self._call(name, self._h, *args, self.n_pages, ctypes.cast(arr, ctypes.c_void_p), ctypes.byref(n))
+        return [(arr[2 * i], arr[2 * i + 1]) for i in range(n.value)]
+
+    def open(self) -> int:
+        """A new, empty sequence."""
+        return self._number("open")
+
+    def fork(self, seq: int) -> int:
+        """A new sequence that shares the pages of ``seq``."""
+        return self._number("fork", int(seq))
+
+    def reserve(self, seq: int, start: int, stop: int) -> List[Tuple[int, int]]:
+        """Own pages for positions ``start`` to ``stop`` - 1; returns the page copies to make before they are written."""
+        return self._pairs("reserve", int(seq), int(start), int(stop))
+
+    def truncate(self, seq: int, length: int) -> None:
+        self._call("truncate", self._h, int(seq), int(length))
+
+    def free(self, seq: int) -> None:
+        """Give back all pages of the sequence, and its number."""
+        self._call("close", self._h, int(seq))
+
+    def pages(self, seq: int) -> List[int]:
+        """The row of the page table."""
+        arr, n = (ctypes.c_int32 * self.n_pages)(), ctypes.c_int32(0)
+        self._call("list", self._h, int(seq), self.n_pages, ctypes.cast(arr, ctypes.c_void_p), ctypes.byref(n))
+        return list(arr)[:n.value]
+
+    def free_pages(self) -> int:
+        return self._number("free_count")
+
+    def compact(self) -> List[Tuple[int, int]]:
+        """Move the pages in use to the lowest numbers; returns the page copies to make."""
+        return self._pairs("compact")
+
+    def close(self) -> None:
+        if getattr(self, "_h", None) is not None and self._h.value:
+            self._lib.s2moe_pages_destroy(self._h)
             self._h = ctypes.c_void_p(None)
 
     def __del__(self):

@@ -4,14 +4,15 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libs2moe.so")
-SOURCES = ["s2moe_api.cu"]
+SOURCES = ["s2moe_api.cu", "attn_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--use_fast_math", "-Xcompiler", "-fPIC", "-shared",
+    "--use_fast_math", "-Xcompiler", "-fPIC",
 ]
 
 
@@ -32,9 +33,17 @@ def _stale() -> bool:
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """Build ``libs2moe.so`` next to this file if it is missing or out of date."""
     if force or _stale():
-        cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else [])
-        cmd += ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-        subprocess.check_call(cmd)
+        # one object per source, compiled beside each other
+        with tempfile.TemporaryDirectory() as tmp:
+            objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+            base = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else [])
+            running = [subprocess.Popen(base + ["-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, objects)]
+            for p in running:
+                p.wait()
+            for p in running:
+                if p.returncode:
+                    raise subprocess.CalledProcessError(p.returncode, p.args)
+            subprocess.check_call([_nvcc()] + NVCC_FLAGS + ["-shared", "-o", LIB] + objects)
     return LIB
 
 

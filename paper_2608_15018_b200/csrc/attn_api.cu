@@ -1,0 +1,449 @@
+// C ABI of the attention calls and of the paged key/value cache: validation and dispatch.
+// See include/s2moe.h for the contract of every entry point.
+#include "../../include/s2moe.h"
+
+#include <cuda_runtime.h>
+
+#include <new>
+#include <vector>
+
+#include "attn_common.cuh"
+#include "attn_simple.cuh"
+#include "kv_cache.cuh"
+#include "page_pool.h"
+
+using namespace s2moe;
+
+struct s2moe_pages {
+    PagePool pool;
+    s2moe_pages(int pages, int size) : pool(pages, size) {}
+};
+
+namespace {
+
+__device__ int g_attn_status;
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+int elem_size(int dtype) { return dtype == S2MOE_F32 ? 4 : 2; }
+bool head_dim_ok(int d) { return d == 64 || d == 128; }
+
+int *status_word()
+{
+    void *p = nullptr;
+    return cudaGetSymbolAddress(&p, g_attn_status) == cudaSuccess ? static_cast<int *>(p) : nullptr;
+}
+
+int sm_count()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return n;
+}
+
+// 0 or a negative status
+int check_cache(const s2moe_kv_cache *c)
+{
+    if (!c || !c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return S2MOE_EINVAL;
+    if (c->dtype != S2MOE_F32 && c->dtype != S2MOE_BF16) return S2MOE_EINVAL;
+    if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || !head_dim_ok(c->head_dim)) return S2MOE_EINVAL;
+    if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return S2MOE_EINVAL;
+    // rows are counted in 32 bits per layer, bytes in 64
+    if ((int64_t)c->n_pages * c->n_kv_heads * c->page_size > INT32_MAX) return S2MOE_ERANGE;
+    return S2MOE_OK;
+}
+
+int page_shift(int size) { return size == 16 ? 4 : size == 32 ? 5 : size == 64 ? 6 : 7; }
+
+KvShape kv_shape(const s2moe_kv_cache *c)
+{
+    return KvShape{c->n_layers, c->n_pages, c->n_kv_heads, page_shift(c->page_size), c->head_dim * elem_size(c->dtype) / 16};
+}
+
+bool heads_ok(int n_heads, int n_kv_heads)
+{
+    return n_heads >= 1 && n_kv_heads >= 1 && n_heads % n_kv_heads == 0 && n_heads / n_kv_heads <= S2MOE_ATTN_MAX_GROUP;
+}
+
+int launch_status() { return cudaGetLastError() == cudaSuccess ? S2MOE_OK : S2MOE_ECUDA; }
+
+// The launch plan of a tree attention call: a function of what the host knows, the same in the call and in the
+// workspace query.
+struct TreePlan {
+    int rows_tile, grid, min_units, key_tile;
+    bool split;
+    int64_t items;                 // upper bound
+    int64_t workspace;
+};
+
+TreePlan tree_plan(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_heads, int head_dim, int64_t capacity, int n_sm)
+{
+    TreePlan p{};
+    const int group = n_heads / n_kv_heads;
+    (void)dtype;
+    // rows of one sequence at most: trees with parents have up to 64 tokens, chains any number
+    const int64_t rows = (int64_t)n_tokens * group;
+    p.rows_tile = rows <= 16 ? 16 : 64;
+    p.key_tile = kAttnSimpleTile;
+    p.min_units = 4;
+    p.items = (int64_t)n_kv_heads * (rows / p.rows_tile + (n_tokens < n_seq ? n_tokens : n_seq));
+    p.split = capacity > (int64_t)p.min_units * p.key_tile;
+    p.grid = 2 * n_sm;
+    p.workspace = p.split ? (int64_t)p.grid * 2 * p.rows_tile * (head_dim + 2) * 4 : 0;
+    return p;
+}
+
+template <typename K, typename... A>
+int launch(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, bool behind, A... args)
+{
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        return S2MOE_ECUDA;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)grid);
+    lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    lc.attrs = &attr;
+    lc.numAttrs = behind ? 1 : 0;
+    return cudaLaunchKernelEx(&lc, kernel, args...) == cudaSuccess ? S2MOE_OK : S2MOE_ECUDA;
+}
+
+template <typename T, int D, int R, bool PAGED, bool SPLIT>
+int launch_simple(const AttnArgs &a, int64_t grid, cudaStream_t st)
+{
+    return launch(attn_simple_kernel<T, D, R, PAGED, SPLIT>, grid, kAttnSimpleThreads, (size_t)attn_simple_smem(D, R), st, false, a);
+}
+
+template <typename T, int D>
+int run_prompt(AttnArgs a, cudaStream_t st)
+{
+    a.rows_tile = 64;
+    int64_t items = (int64_t)a.Hk * ((int64_t)a.n_tokens * a.group / 64 + a.n_seq);
+    if (items > (1 << 20)) items = 1 << 20;
+    return launch_simple<T, D, 64, false, false>(a, items, st);
+}
+
+template <typename T, int D>
+int run_tree(AttnArgs a, const TreePlan &p, cudaStream_t st)
+{
+    a.rows_tile = p.rows_tile;
+    a.min_units = p.min_units;
+    if (!p.split) {
+        const int64_t items = p.items < (1 << 20) ? p.items : 1 << 20;
+        return p.rows_tile == 16 ? launch_simple<T, D, 16, true, false>(a, items, st) : launch_simple<T, D, 64, true, false>(a, items, st);
+    }
+    const int rc = p.rows_tile == 16 ? launch_simple<T, D, 16, true, true>(a, p.grid, st) : launch_simple<T, D, 64, true, true>(a, p.grid, st);
+    if (rc != S2MOE_OK) return rc;
+    return launch(attn_join_kernel<T, D, kAttnSimpleTile>, ((int64_t)a.n_tokens * a.Hk + 3) / 4, 128, 0, st, true, a, p.grid);
+}
+
+}  // namespace
+
+extern "C" {
+
+int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                           const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                           const int32_t *seq_start, float scale, void *out, void *cuda_stream)
+{
+    if (dtype != S2MOE_F32 && dtype != S2MOE_BF16) return S2MOE_EINVAL;
+    if (n_seq < 0 || n_tokens < 0 || !heads_ok(n_heads, n_kv_heads) || !head_dim_ok(head_dim)) return S2MOE_EINVAL;
+    if (!(scale >= 0.f && scale <= 1e30f)) return S2MOE_EINVAL;
+    if (n_seq == 0 || n_tokens == 0) return S2MOE_OK;
+    if (!q || !k || !v || !seq_start || !out) return S2MOE_EINVAL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return S2MOE_EINVAL;
+    const int per16 = 16 / elem_size(dtype);
+    if (q_stride % per16 || k_stride % per16 || v_stride % per16) return S2MOE_EINVAL;
+    if (q_stride < (int64_t)n_heads * head_dim || k_stride < (int64_t)n_kv_heads * head_dim || v_stride < (int64_t)n_kv_heads * head_dim)
+        return S2MOE_EINVAL;
+    if ((int64_t)n_tokens * n_heads > INT32_MAX) return S2MOE_ERANGE;
+    AttnArgs a{};
+    a.q = q; a.k = k; a.v = v; a.out = out;
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+    a.seq_start = seq_start;
+    a.n_seq = n_seq; a.n_tokens = a.n_nodes = n_tokens; a.Hk = n_kv_heads; a.group = n_heads / n_kv_heads;
+    a.min_units = 1;
+    a.scale_log2 = scale * 1.44269504f;
+    a.status = status_word();
+    if (!a.status) return S2MOE_ECUDA;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == S2MOE_F32) return head_dim == 64 ? run_prompt<float, 64>(a, st) : run_prompt<float, 128>(a, st);
+    return head_dim == 64 ? run_prompt<__nv_bfloat16, 64>(a, st) : run_prompt<__nv_bfloat16, 128>(a, st);
+}
+
+int s2moe_tree_attention_workspace(const s2moe_kv_cache *cache, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t table_width,
+                                   int64_t *bytes)
+{
+    if (!bytes) return S2MOE_EINVAL;
+    *bytes = 0;
+    const int rc = check_cache(cache);
+    if (rc != S2MOE_OK) return rc;
+    if (n_seq < 0 || n_tokens < 0 || table_width < 1 || !heads_ok(n_heads, cache->n_kv_heads)) return S2MOE_EINVAL;
+    if (n_seq == 0 || n_tokens == 0) return S2MOE_OK;
+    const int n_sm = sm_count();
+    if (n_sm < 1) return S2MOE_ECUDA;
+    *bytes = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads, cache->head_dim, (int64_t)table_width * cache->page_size,
+                       n_sm).workspace;
+    return S2MOE_OK;
+}
+
+int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, int32_t n_heads, const void *q,
+                         int64_t q_stride, const int32_t *page_table, int32_t table_width, const int32_t *context,
+                         const int32_t *seq_start, int32_t n_nodes, const int32_t *node_start, const int32_t *parent, float scale,
+                         void *out, void *workspace, int64_t workspace_bytes, void *cuda_stream)
+{
+    const int rc = check_cache(cache);
+    if (rc != S2MOE_OK) return rc;
+    if (layer < 0 || layer >= cache->n_layers) return S2MOE_ERANGE;
+    if (n_seq < 0 || n_tokens < 0 || n_nodes < 0 || table_width < 1 || !heads_ok(n_heads, cache->n_kv_heads)) return S2MOE_EINVAL;
+    if (!(scale >= 0.f && scale <= 1e30f)) return S2MOE_EINVAL;
+    if (!node_start && n_nodes != n_tokens) return S2MOE_EINVAL;
+    if (n_seq == 0 || n_tokens == 0) return S2MOE_OK;
+    if (!q || !page_table || !context || !seq_start || !out) return S2MOE_EINVAL;
+    if (!aligned16(q) || !aligned16(out) || q_stride % (16 / elem_size(cache->dtype)) || q_stride < (int64_t)n_heads * cache->head_dim)
+        return S2MOE_EINVAL;
+    if ((int64_t)n_tokens * n_heads > INT32_MAX || (int64_t)table_width * cache->page_size > INT32_MAX - 128) return S2MOE_ERANGE;
+    const int n_sm = sm_count();
+    if (n_sm < 1) return S2MOE_ECUDA;
+    const TreePlan p = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads, cache->head_dim,
+                                 (int64_t)table_width * cache->page_size, n_sm);
+    if (p.workspace > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < p.workspace)) return S2MOE_EINVAL;
+    const int64_t layer_bytes = (int64_t)cache->n_pages * cache->n_kv_heads * cache->page_size * cache->head_dim * elem_size(cache->dtype);
+    AttnArgs a{};
+    a.q = q;
+    a.k = (const uint8_t *)cache->k + layer * layer_bytes;
+    a.v = (const uint8_t *)cache->v + layer * layer_bytes;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.seq_start = seq_start; a.node_start = node_start; a.context = context; a.parent = parent; a.page_table = page_table;
+    a.n_seq = n_seq; a.n_tokens = n_tokens; a.n_nodes = n_nodes;
+    a.Hk = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads;
+    a.table_width = table_width; a.page_shift = page_shift(cache->page_size); a.n_pages = cache->n_pages;
+    a.scale_log2 = scale * 1.44269504f;
+    a.part_o = (float *)workspace;
+    a.part_ml = (float *)workspace + (int64_t)p.grid * 2 * p.rows_tile * cache->head_dim;
+    a.status = status_word();
+    if (!a.status) return S2MOE_ECUDA;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const bool wide = cache->head_dim == 128;
+    if (cache->dtype == S2MOE_F32) return wide ? run_tree<float, 128>(a, p, st) : run_tree<float, 64>(a, p, st);
+    return wide ? run_tree<__nv_bfloat16, 128>(a, p, st) : run_tree<__nv_bfloat16, 64>(a, p, st);
+}
+
+int s2moe_attention_status(int32_t *host_out)
+{
+    if (!host_out) return S2MOE_EINVAL;
+    *host_out = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess) return S2MOE_ECUDA;
+    if (cudaMemcpyFromSymbol(host_out, g_attn_status, sizeof(int32_t)) != cudaSuccess) return S2MOE_ECUDA;
+    if (*host_out == 0) return S2MOE_OK;
+    const int32_t zero = 0;
+    return cudaMemcpyToSymbol(g_attn_status, &zero, sizeof(zero)) == cudaSuccess ? S2MOE_ETIMEOUT : S2MOE_ECUDA;
+}
+
+// ---- the cache ----------------------------------------------------------------------------------------------------
+
+int s2moe_kv_write(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, const void *k, int64_t k_stride,
+                   const void *v, int64_t v_stride, const int32_t *page_table, int32_t table_width, const int32_t *first,
+                   const int32_t *seq_start, void *cuda_stream)
+{
+    const int rc = check_cache(cache);
+    if (rc != S2MOE_OK) return rc;
+    if (layer < 0 || layer >= cache->n_layers) return S2MOE_ERANGE;
+    if (n_seq < 0 || n_tokens < 0 || table_width < 1) return S2MOE_EINVAL;
+    if (n_seq == 0 || n_tokens == 0) return S2MOE_OK;
+    if (!k || !v || !page_table || !first || !seq_start || !aligned16(k) || !aligned16(v)) return S2MOE_EINVAL;
+    const int es = elem_size(cache->dtype);
+    const int64_t row = (int64_t)cache->n_kv_heads * cache->head_dim;
+    if (k_stride < row || v_stride < row || k_stride * es % 16 || v_stride * es % 16) return S2MOE_EINVAL;
+    KvWriteArgs a{};
+    a.c = kv_shape(cache);
+    a.dst[0] = (uint4 *)cache->k; a.dst[1] = (uint4 *)cache->v;
+    a.src[0] = (const uint4 *)k; a.src[1] = (const uint4 *)v;
+    a.stride[0] = k_stride * es / 16; a.stride[1] = v_stride * es / 16;
+    a.seq_start = seq_start; a.first = first; a.page_table = page_table;
+    a.layer = layer; a.n_seq = n_seq; a.n_tokens = n_tokens; a.table_width = table_width;
+    kv_write_kernel<<<dim3((unsigned)((n_tokens + 3ll) / 4), 2), 128, 0, (cudaStream_t)cuda_stream>>>(a);
+    return launch_status();
+}
+
+int s2moe_kv_commit(const s2moe_kv_cache *cache, int32_t n_seq, const int32_t *page_table, int32_t table_width, const int32_t *context,
+                    const int32_t *path, int32_t max_path, const int32_t *n_path, int32_t *new_context, void *cuda_stream)
+{
+    const int rc = check_cache(cache);
+    if (rc != S2MOE_OK) return rc;
+    if (n_seq < 0 || table_width < 1 || max_path < 1) return S2MOE_EINVAL;
+    if (max_path > kKvMaxPath) return S2MOE_ERANGE;
+    if (n_seq == 0) return S2MOE_OK;
+    if (!page_table || !context || !path || !n_path || !new_context) return S2MOE_EINVAL;
+    // other blocks still read the contexts while one writes the new ones
+    if (new_context < context + n_seq && context < new_context + n_seq) return S2MOE_EINVAL;
+    KvCommitArgs a{};
+    a.c = kv_shape(cache);
+    a.pool[0] = (uint4 *)cache->k; a.pool[1] = (uint4 *)cache->v;
+    a.page_table = page_table; a.context = context; a.path = path; a.n_path = n_path; a.new_context = new_context;
+    a.n_seq = n_seq; a.table_width = table_width; a.max_path = max_path;
+    const int64_t per_seq = (int64_t)cache->n_layers * 2 * ((cache->n_kv_heads * a.c.row16 + 31) / 32);
+    if (per_seq > 65535) return S2MOE_ERANGE;
+    kv_commit_kernel<<<dim3((unsigned)n_seq, (unsigned)per_seq), 32, 0, (cudaStream_t)cuda_stream>>>(a);
+    return launch_status();
+}
+
+int s2moe_kv_copy_pages(const s2moe_kv_cache *cache, int32_t n_pairs, const int32_t *pairs, void *cuda_stream)
+try {
+    const int rc = check_cache(cache);
+    if (rc != S2MOE_OK) return rc;
+    if (n_pairs < 0) return S2MOE_EINVAL;
+    if (n_pairs == 0) return S2MOE_OK;
+    if (!pairs) return S2MOE_EINVAL;
+    // the copies run beside each other: no page may be written twice, or written and read
+    std::vector<uint8_t> use((size_t)cache->n_pages, 0);
+    for (int i = 0; i < n_pairs; ++i) {
+        const int src = pairs[2 * i], dst = pairs[2 * i + 1];
+        if (src < 0 || src >= cache->n_pages || dst < 0 || dst >= cache->n_pages) return S2MOE_ERANGE;
+        if (use[(size_t)dst] || (use[(size_t)src] & 2) || src == dst) return S2MOE_EINVAL;
+        use[(size_t)src] |= 1;
+        use[(size_t)dst] |= 2;
+    }
+    if (cache->n_layers > 32767) return S2MOE_ERANGE;
+    KvCopyArgs a{};
+    a.pool[0] = (uint4 *)cache->k; a.pool[1] = (uint4 *)cache->v;
+    const KvShape c = kv_shape(cache);
+    a.page16 = ((int64_t)c.heads * c.row16) << c.page_shift;
+    a.n_pages = c.n_pages;
+    const int64_t pieces = (a.page16 + kKvCopyWords - 1) / kKvCopyWords;
+    for (int done = 0; done < n_pairs; done += kKvPairs) {
+        const int n = n_pairs - done < kKvPairs ? n_pairs - done : kKvPairs;
+        for (int i = 0; i < n; ++i) {
+            a.pair[i][0] = pairs[2 * (done + i)];
+            a.pair[i][1] = pairs[2 * (done + i) + 1];
+        }
+        kv_copy_kernel<<<dim3((unsigned)pieces, (unsigned)n, (unsigned)(2 * c.layers)), kKvCopyThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+        const int lrc = launch_status();
+        if (lrc != S2MOE_OK) return lrc;
+    }
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+// ---- pages (host only) ----------------------------------------------------------------------------------------------
+
+int s2moe_pages_create(int32_t n_pages, int32_t page_size, s2moe_pages **out)
+try {
+    if (!out) return S2MOE_EINVAL;
+    *out = nullptr;
+    if (n_pages < 1 || page_size < 1) return S2MOE_EINVAL;
+    *out = new s2moe_pages(n_pages, page_size);
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+int s2moe_pages_destroy(s2moe_pages *pages)
+{
+    delete pages;
+    return S2MOE_OK;
+}
+
+int s2moe_pages_open(s2moe_pages *pages, int32_t *seq_out)
+try {
+    if (!pages || !seq_out) return S2MOE_EINVAL;
+    *seq_out = pages->pool.open();
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+int s2moe_pages_fork(s2moe_pages *pages, int32_t seq, int32_t *seq_out)
+try {
+    if (!pages || !seq_out) return S2MOE_EINVAL;
+    if (!pages->pool.known(seq)) return S2MOE_ERANGE;
+    *seq_out = pages->pool.fork(seq);
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+int s2moe_pages_reserve(s2moe_pages *pages, int32_t seq, int64_t from, int64_t to, int32_t max_pairs, int32_t *pairs_out,
+                        int32_t *n_pairs_out)
+try {
+    if (!pages || !n_pairs_out || max_pairs < 0 || (max_pairs > 0 && !pairs_out)) return S2MOE_EINVAL;
+    *n_pairs_out = 0;
+    PagePool &pool = pages->pool;
+    if (!pool.known(seq)) return S2MOE_ERANGE;
+    if (from < 0 || to < from) return S2MOE_EINVAL;
+    if (to > (int64_t)pool.n_pages * pool.page_size) return S2MOE_ENOMEM;
+    const int need = pool.copies_needed(seq, from, to);
+    if (need > max_pairs) {
+        *n_pairs_out = need;
+        return S2MOE_ERANGE;
+    }
+    std::vector<std::pair<int32_t, int32_t>> copies;
+    if (!pool.reserve(seq, from, to, copies)) return S2MOE_ENOMEM;
+    for (size_t i = 0; i < copies.size(); ++i) {
+        pairs_out[2 * i] = copies[i].first;
+        pairs_out[2 * i + 1] = copies[i].second;
+    }
+    *n_pairs_out = (int32_t)copies.size();
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+int s2moe_pages_truncate(s2moe_pages *pages, int32_t seq, int64_t length)
+try {
+    if (!pages || length < 0) return S2MOE_EINVAL;
+    if (!pages->pool.known(seq)) return S2MOE_ERANGE;
+    pages->pool.truncate(seq, length);
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+int s2moe_pages_close(s2moe_pages *pages, int32_t seq)
+try {
+    if (!pages) return S2MOE_EINVAL;
+    if (!pages->pool.known(seq)) return S2MOE_ERANGE;
+    pages->pool.close(seq);
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+int s2moe_pages_list(const s2moe_pages *pages, int32_t seq, int32_t max_pages, int32_t *pages_out, int32_t *n_pages_out)
+{
+    if (!pages || !n_pages_out || max_pages < 0 || (max_pages > 0 && !pages_out)) return S2MOE_EINVAL;
+    *n_pages_out = 0;
+    if (!pages->pool.known(seq)) return S2MOE_ERANGE;
+    const std::vector<int32_t> &list = pages->pool.seqs[(size_t)seq];
+    *n_pages_out = (int32_t)list.size();
+    for (size_t i = 0; i < list.size() && (int64_t)i < max_pages; ++i) pages_out[i] = list[i];
+    return (int64_t)list.size() > max_pages ? S2MOE_ERANGE : S2MOE_OK;
+}
+
+int s2moe_pages_free_count(const s2moe_pages *pages, int32_t *out)
+{
+    if (!pages || !out) return S2MOE_EINVAL;
+    *out = (int32_t)pages->pool.free_pages.size();
+    return S2MOE_OK;
+}
+
+int s2moe_pages_compact(s2moe_pages *pages, int32_t max_pairs, int32_t *pairs_out, int32_t *n_pairs_out)
+try {
+    if (!pages || !n_pairs_out || max_pairs < 0 || (max_pairs > 0 && !pairs_out)) return S2MOE_EINVAL;
+    *n_pairs_out = pages->pool.moves_needed();
+    if (*n_pairs_out > max_pairs) return S2MOE_ERANGE;
+    std::vector<std::pair<int32_t, int32_t>> copies;
+    pages->pool.compact(copies);
+    for (size_t i = 0; i < copies.size(); ++i) {
+        pairs_out[2 * i] = copies[i].first;
+        pairs_out[2 * i + 1] = copies[i].second;
+    }
+    return S2MOE_OK;
+} catch (...) {
+    return S2MOE_ENOMEM;
+}
+
+}  // extern "C"

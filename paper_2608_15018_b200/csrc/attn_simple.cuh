@@ -1,0 +1,304 @@
+// Attention on the CUDA cores, for every type (binary32 runs on it), and the kernel that joins the pieces of split items.
+//
+// A CTA of 256 threads holds R rows of q and takes the keys 64 at a time: scores by register tiles of R/16 rows x 4
+// keys per thread, the running maximum m and sum l of the softmax (p = 2^(s - m), l' = l 2^(m - m') + sum p, likewise
+// the product), then the product with the values by register tiles of R/16 rows x D/16 columns.  All of it in
+// binary32.
+#pragma once
+
+#include "attn_common.cuh"
+
+namespace s2moe {
+
+constexpr int kAttnSimpleThreads = 256;
+constexpr int kAttnSimpleTile = 64;       // keys of a tile
+
+__host__ __device__ constexpr int attn_simple_smem(int D, int R)
+{
+    // q rows, then the tile's keys (whose place the weights take once the scores are known), then its values
+    return 4 * (R * (D + 4) + (64 * (D + 4) > R * 68 ? 64 * (D + 4) : R * 68) + 64 * D);
+}
+
+template <typename T>
+__device__ __forceinline__ float4 attn_load4(const T *p);
+template <>
+__device__ __forceinline__ float4 attn_load4<float>(const float *p) { return __ldg(reinterpret_cast<const float4 *>(p)); }
+template <>
+__device__ __forceinline__ float4 attn_load4<__nv_bfloat16>(const __nv_bfloat16 *p)
+{
+    const uint2 w = __ldg(reinterpret_cast<const uint2 *>(p));
+    return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+}
+__device__ __forceinline__ void attn_store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void attn_store4(__nv_bfloat16 *p, float4 v)
+{
+    __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(reinterpret_cast<uint32_t &>(lo), reinterpret_cast<uint32_t &>(hi));
+}
+
+// The rows of `again` lanes (bit per lane) once more, one by one by the whole warp; each lane names its own row.
+template <typename T, int D, bool PAGED>
+__device__ __forceinline__ void attn_fix_rows(const AttnArgs &a, const AttnSeq &q, int s, int h, unsigned again, int token, int head,
+                                              int kend, bool no_weight)
+{
+    const int lane = threadIdx.x & 31;
+    while (again) {
+        const int l = __ffs((int)again) - 1;
+        again &= again - 1;
+        const int tk = __shfl_sync(0xffffffffu, token, l), hd = __shfl_sync(0xffffffffu, head, l);
+        const bool nw = __shfl_sync(0xffffffffu, (int)no_weight, l) != 0;
+        float o[D / 32];
+        if (attn_row_again<T, D, PAGED>(a, q, s, h, tk, hd, kend, nw, o)) {
+            T *dst = reinterpret_cast<T *>(a.out) + ((long long)(q.tok0 + tk) * a.Hk * a.group + hd) * D;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) dst[lane + 32 * i] = (T)o[i];
+        }
+        __syncwarp();
+    }
+}
+
+template <typename T, int D, int R, bool PAGED, bool SPLIT>
+__global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(AttnArgs a)
+{
+    constexpr int RT = R / 16, CT = D / 64, QP = D + 4, PP = 68;
+    extern __shared__ __align__(16) float attn_smem[];
+    float *qs = attn_smem, *ks = qs + R * QP, *ps = ks, *vs = ks + (64 * QP > R * PP ? 64 * QP : R * PP);
+    __shared__ int key_ok[64];
+    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
+    if (SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // the joining kernel waits for the end
+    AttnIter<PAGED, SPLIT, kAttnSimpleTile> it(a, lane);
+    AttnPiece p;
+    it.begin();
+    while (it.next(p)) {
+        const AttnSeq &q = p.q;
+        const int rows = q.n * a.group, row0 = p.rt * R;
+        __syncthreads();
+        for (int i = tid; i < R * (D / 4); i += kAttnSimpleThreads) {
+            const int r = i / (D / 4), c = i % (D / 4) * 4, row = row0 + r;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row < rows) {
+                const int t = row / a.group, head = p.h * a.group + row % a.group;
+                x = attn_load4(reinterpret_cast<const T *>(a.q) + (long long)(q.tok0 + t) * a.q_stride + (long long)head * D + c);
+            }
+            attn_store4(qs + r * QP + c, x);
+        }
+        int lim[RT];
+        unsigned long long anc[RT];
+        float m[RT], l[RT], o[RT][4 * CT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int row = row0 + ty + 16 * i;
+            lim[i] = 0;
+            anc[i] = ~0ull;
+            if (row < rows) {
+                lim[i] = attn_limit<PAGED>(q, row / a.group);
+                if (PAGED && a.parent && !q.bad) anc[i] = attn_ancestors(a, q, q.nodes - q.n + row / a.group);
+            }
+            m[i] = -CUDART_INF_F;
+            l[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4 * CT; ++c) o[i][c] = 0.f;
+        }
+        for (int t = p.t0; t < p.t1; ++t) {
+            __syncthreads();
+            {
+                const int r = tid >> 2, key = t * 64 + r;
+                long long ko = 0, vo = 0;
+                const bool ok = key < q.total && attn_key<PAGED, D>(a, q, p.s, p.h, key, ko, vo);
+                if ((tid & 3) == 0) key_ok[r] = ok;
+#pragma unroll 4
+                for (int c = (tid & 3) * 4; c < D; c += 16) {
+                    float4 kk = make_float4(0.f, 0.f, 0.f, 0.f), vv = kk;
+                    if (ok) {
+                        kk = attn_load4(reinterpret_cast<const T *>(a.k) + ko + c);
+                        vv = attn_load4(reinterpret_cast<const T *>(a.v) + vo + c);
+                    }
+                    attn_store4(ks + r * QP + c, kk);
+                    attn_store4(vs + r * D + c, vv);
+                }
+            }
+            __syncthreads();
+            float sc[RT][4];
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sc[i][j] = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < D; c += 4) {
+                float4 kk[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) kk[j] = *reinterpret_cast<const float4 *>(ks + (tx + 16 * j) * QP + c);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const float4 x = *reinterpret_cast<const float4 *>(qs + (ty + 16 * i) * QP + c);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        sc[i][j] = fmaf(x.x, kk[j].x, fmaf(x.y, kk[j].y, fmaf(x.z, kk[j].z, fmaf(x.w, kk[j].w, sc[i][j]))));
+                }
+            }
+            bool ok[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ok[j] = key_ok[tx + 16 * j] != 0;
+            __syncthreads();                     // the weights go where the keys are
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                float mx = -CUDART_INF_F;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool sees = ok[j] && attn_sees(t * 64 + tx + 16 * j, q.ctx, lim[i], anc[i]);
+                    sc[i][j] = sees ? sc[i][j] * a.scale_log2 : -CUDART_INF_F;
+                    mx = fmaxf(mx, sc[i][j]);
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                const float mn = fmaxf(m[i], mx), base = mn == -CUDART_INF_F ? 0.f : mn;
+                const float f = exp2f(m[i] - base);
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float w = exp2f(sc[i][j] - base);
+                    sum += w;
+                    ps[(ty + 16 * i) * PP + tx + 16 * j] = w;
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                l[i] = l[i] * f + sum;
+                m[i] = mn;
+#pragma unroll
+                for (int c = 0; c < 4 * CT; ++c) o[i][c] *= f;
+            }
+            __syncwarp();                        // a row's weights are written and read by one half warp
+#pragma unroll 4
+            for (int j = 0; j < 64; j += 4) {
+                float4 w[RT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) w[i] = *reinterpret_cast<const float4 *>(ps + (ty + 16 * i) * PP + j);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    float4 vv[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) vv[x] = *reinterpret_cast<const float4 *>(vs + (j + x) * D + 64 * c + 4 * tx);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        float *oo = &o[i][4 * c];
+                        oo[0] = fmaf(w[i].x, vv[0].x, fmaf(w[i].y, vv[1].x, fmaf(w[i].z, vv[2].x, fmaf(w[i].w, vv[3].x, oo[0]))));
+                        oo[1] = fmaf(w[i].x, vv[0].y, fmaf(w[i].y, vv[1].y, fmaf(w[i].z, vv[2].y, fmaf(w[i].w, vv[3].y, oo[1]))));
+                        oo[2] = fmaf(w[i].x, vv[0].z, fmaf(w[i].y, vv[1].z, fmaf(w[i].z, vv[2].z, fmaf(w[i].w, vv[3].z, oo[2]))));
+                        oo[3] = fmaf(w[i].x, vv[0].w, fmaf(w[i].y, vv[1].w, fmaf(w[i].z, vv[2].w, fmaf(w[i].w, vv[3].w, oo[3]))));
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int r = ty + 16 * i, row = row0 + r;
+            const bool mine = row < rows;
+            const int token = mine ? row / a.group : 0, head = p.h * a.group + (mine ? row % a.group : 0);
+            if (SPLIT && p.slot >= 0) {
+                if (mine) {
+                    const long long at = (long long)p.slot * R + r;
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+                        attn_store4(a.part_o + at * D + 64 * c + 4 * tx, make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]));
+                    if (tx == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m[i], l[i]);
+                }
+                continue;
+            }
+            const float inv = q.bad ? CUDART_NAN_F : 1.f / l[i];
+            bool fine = true;
+            if (mine) {
+                T *dst = reinterpret_cast<T *>(a.out) + ((long long)(q.tok0 + token) * a.Hk * a.group + head) * D;
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const float4 v = make_float4(o[i][4 * c] * inv, o[i][4 * c + 1] * inv, o[i][4 * c + 2] * inv, o[i][4 * c + 3] * inv);
+                    fine = fine && attn_finite(v.x) && attn_finite(v.y) && attn_finite(v.z) && attn_finite(v.w);
+                    attn_store4(dst + 64 * c + 4 * tx, v);
+                }
+            }
+            // the two rows of a warp: a half warp each
+            const unsigned bad = __ballot_sync(0xffffffffu, mine && !q.bad && !fine);
+            const unsigned again = (bad & 0xffffu ? 1u : 0u) | (bad >> 16 ? 1u << 16 : 0u);
+            if (again) {
+                __syncwarp();
+                attn_fix_rows<T, D, PAGED>(a, q, p.s, p.h, again, token, head, p.t1 * 64, l[i] == 0.f);
+            }
+        }
+    }
+}
+
+// Joins the pieces of the items that the split cut: one warp per token and key/value head.
+//   M = max m_i, out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M)
+template <typename T, int D, int KEY_TILE>
+__global__ void __launch_bounds__(128) attn_join_kernel(AttnArgs a, int grid)
+{
+    using Cut = AttnCut<KEY_TILE>;
+    constexpr int C = D / 32;
+    const int lane = threadIdx.x & 31;
+    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int tok = (int)(unit / a.Hk), h = (int)(unit - (long long)tok * a.Hk);
+    AttnIter<true, true, KEY_TILE> it(a, lane);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (tok >= a.n_tokens) return;
+    const long long w = it.total_units(), g = it.ctas(a, w, grid);
+    // the sequence of this token, and the units in front of it
+    long long base = 0;
+    int s = -1;
+    for (int s0 = 0; s0 < a.n_seq && s < 0; s0 += 32) {
+        long long un = 0;
+        bool mine = false;
+        if (s0 + lane < a.n_seq) {
+            const AttnSeq x = attn_seq<true>(a, s0 + lane);
+            mine = tok >= x.tok0 && tok < x.tok0 + x.n;
+            un = it.units_of(s0 + lane);
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, mine);
+        if (hit) s = s0 + __ffs((int)hit) - 1;
+        if (hit && lane >= __ffs((int)hit) - 1) un = 0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) un += __shfl_xor_sync(0xffffffffu, un, o);
+        base += un;
+    }
+    if (s < 0) return;
+    const AttnSeq q = attn_seq<true>(a, s);
+    const int tiles = Cut::tiles(q), rts = Cut::row_tiles(a, q), t = tok - q.tok0;
+    for (int gr = 0; gr < a.group; ++gr) {
+        const int row = t * a.group + gr, rt = row / a.rows_tile, r = row - rt * a.rows_tile;
+        const long long u0 = base + ((long long)h * rts + rt) * tiles, u1 = u0 + tiles;
+        const long long c0 = ((u0 + 1) * g - 1) / w, c1 = (u1 * g - 1) / w;       // CTAs of the first and the last unit
+        if (c0 == c1) continue;                                                // a whole item: written already
+        float m = -CUDART_INF_F, l = 0.f, o[C];
+#pragma unroll
+        for (int i = 0; i < C; ++i) o[i] = 0.f;
+        for (long long c = c0; c <= c1; ++c) {
+            const long long slot = 2 * c + (c == c0 && w * c / g < u0 ? 1 : 0);
+            const long long at = slot * a.rows_tile + r;
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
+            const float mn = fmaxf(m, ml.x), b = mn == -CUDART_INF_F ? 0.f : mn;
+            const float f = exp2f(m - b), e = exp2f(ml.x - b);
+            m = mn;
+            l = l * f + ml.y * e;
+#pragma unroll
+            for (int i = 0; i < C; ++i) o[i] = o[i] * f + a.part_o[at * D + lane + 32 * i] * e;
+        }
+        const int head = h * a.group + gr;
+        const float inv = q.bad ? CUDART_NAN_F : 1.f / l;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            o[i] *= inv;
+            fine = fine && attn_finite(o[i]);
+        }
+        if (!q.bad && __any_sync(0xffffffffu, !fine)) {
+            float x[C];
+            if (attn_row_again<T, D, true>(a, q, s, h, t, head, q.total, l == 0.f, x)) {
+#pragma unroll
+                for (int i = 0; i < C; ++i) o[i] = x[i];
+            }
+        }
+        T *dst = reinterpret_cast<T *>(a.out) + ((long long)tok * a.Hk * a.group + head) * D;
+#pragma unroll
+        for (int i = 0; i < C; ++i) dst[lane + 32 * i] = (T)o[i];
+    }
+}
+
+}  // namespace s2moe

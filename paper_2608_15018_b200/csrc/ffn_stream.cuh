@@ -24,6 +24,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "ptx.cuh"
 
 namespace s2moe {
 
@@ -31,7 +32,6 @@ constexpr int kStConsumerWarps = 7;   // + 1 producer warp = 256 threads, so a t
 constexpr int kStThreads = (kStConsumerWarps + 1) * 32;
 constexpr int kStMaxStages = 8;
 constexpr int kStMaxGroups = kMaxExperts + kMaxShared;
-constexpr unsigned kStSpinLimit = 1u << 20;   // bounded waits: a poll takes between some tens of ns and kMbarSuspendNs, so about a second at most
 constexpr int kStMaxSmem = 232448 - 2048;     // dynamic shared memory the kernel may use
 
 // Per-call plan, computed on the host (st_make_plan) and passed by value.
@@ -137,53 +137,6 @@ inline StPlan st_make_plan(const Shape &sh, int B, int n_sm, int n_slots)
     return p;
 }
 
-// ---- PTX helpers ---------------------------------------------------------------
-
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint64_t *bar, int count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint64_t *bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes)
-                 : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// upper bound in nanoseconds of the time a thread may stay suspended in one try_wait (it wakes when
-// the phase completes): a waiting thread then costs its scheduler next to no issue slots
-constexpr uint32_t kMbarSuspendNs = 1000;
-__device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity), "r"(kMbarSuspendNs)
-        : "memory");
-    return ok != 0;
-}
-// bounded wait; false when it gave up
-__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity)
-{
-    for (unsigned i = 0; i < kStSpinLimit; ++i)
-        if (mbar_try_wait(bar, parity)) return true;
-    return false;
-}
-__device__ __forceinline__ void bulk_g2s(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
-{
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-            smem_u32(dst)),
-        "l"(src), "r"(bytes), "r"(smem_u32(bar))
-        : "memory");
-}
 #ifdef S2MOE_SELFCHECK
 #define ST_BULK(ws, smem0, smem_bytes, dst, src, bytes, bar, g0, gbytes, code)                                      \
     do {                                                                                                           \
@@ -196,23 +149,6 @@ __device__ __forceinline__ void bulk_g2s(void *dst, const void *src, uint32_t by
 #else
 #define ST_BULK(ws, smem0, smem_bytes, dst, src, bytes, bar, g0, gbytes, code) bulk_g2s(dst, src, bytes, bar)
 #endif
-__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
-__device__ __forceinline__ int ld_acquire(const int *p)
-{
-    int v;
-    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                         uint32_t b0, uint32_t b1)
-{
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-        "{%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 template <typename G>
 __device__ __forceinline__ int upper_group1(const G *g, int n, int u)
 {

@@ -1,0 +1,157 @@
+// Kernels that move rows of the paged key/value cache: writing new tokens, committing an accepted path, copying pages.
+// Pages are [layer][page][kv head][place in page][D]; a row (one head of one token) is 128 to 512 bytes.  All of them
+// are bound by HBM: every byte is read once and written once, 16 bytes per thread and access, eight accesses in flight.
+#pragma once
+
+#include "common.cuh"
+
+namespace s2moe {
+
+constexpr int kKvMaxPath = 64;            // accepted tokens of one commit
+constexpr int kKvPairs = 240;             // page pairs of one launch: they travel as kernel arguments
+
+struct KvShape {
+    int layers, n_pages, heads, page_shift, row16;      // row16: 16-byte words of a row
+};
+__device__ __forceinline__ long long kv_row(const KvShape &c, int layer, int page, int head, int at)
+{
+    return ((((long long)layer * c.n_pages + page) * c.heads + head) << c.page_shift) + at;
+}
+
+// One warp per token and matrix (blockIdx.y 0: keys, 1: values).  Tokens that belong to no sequence, positions outside the
+// table and pages outside the cache are left out.
+struct KvWriteArgs {
+    KvShape c;
+    uint4 *dst[2];
+    const uint4 *src[2];
+    long long stride[2];                  // 16-byte words from token to token
+    const int32_t *seq_start, *first, *page_table;
+    int layer, n_seq, n_tokens, table_width;
+};
+__global__ void __launch_bounds__(128) kv_write_kernel(KvWriteArgs a)
+{
+    const int lane = threadIdx.x & 31, mat = blockIdx.y;
+    const int tok = blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (tok >= a.n_tokens) return;
+    int pos = -1, s = -1;
+    for (int s0 = 0; s0 < a.n_seq && s < 0; s0 += 32) {
+        const int i = s0 + lane;
+        int lo = 0, hi = 0;
+        if (i < a.n_seq) {
+            lo = __ldg(a.seq_start + i);
+            hi = __ldg(a.seq_start + i + 1);
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, tok >= lo && tok < hi);
+        if (hit) {
+            const int l = __ffs((int)hit) - 1;
+            s = s0 + l;
+            pos = tok - __shfl_sync(0xffffffffu, lo, l);
+        }
+    }
+    if (s < 0) return;
+    const long long p = (long long)__ldg(a.first + s) + pos;
+    if (p < 0 || p >= ((long long)a.table_width << a.c.page_shift)) return;
+    const int page = __ldg(a.page_table + (long long)s * a.table_width + (p >> a.c.page_shift));
+    if ((unsigned)page >= (unsigned)a.c.n_pages) return;
+    const uint4 *src = a.src[mat] + (long long)tok * a.stride[mat];
+    uint4 *dst = a.dst[mat] + kv_row(a.c, a.layer, page, 0, (int)(p & ((1 << a.c.page_shift) - 1))) * a.c.row16;
+    const int n = a.c.heads * a.c.row16;
+    const long long head_step = (long long)a.c.row16 << a.c.page_shift;
+    for (int i0 = lane; i0 < n; i0 += 256) {
+        uint4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i0 + 32 * j < n) x[j] = __ldcs(src + i0 + 32 * j);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + 32 * j;
+            if (i < n) dst[i / a.c.row16 * head_step + i % a.c.row16] = x[j];
+        }
+    }
+}
+
+// One warp per sequence, layer, matrix and 32 words of a token's row of all heads: a thread reads its word of all accepted
+// rows before it writes any, so that paths in any order, and paths that name a node twice, move what stood there before the
+// call.  Up to 8 rows stay in registers (a path is rarely longer), more go through shared memory.
+struct KvCommitArgs {
+    KvShape c;
+    uint4 *pool[2];
+    const int32_t *page_table, *context, *path, *n_path;
+    int32_t *new_context;
+    int n_seq, table_width, max_path;
+};
+__global__ void __launch_bounds__(32) kv_commit_kernel(KvCommitArgs a)
+{
+    __shared__ uint4 rows[kKvMaxPath][32];
+    __shared__ long long from[kKvMaxPath], to[kKvMaxPath];
+    const int lane = threadIdx.x, s = blockIdx.x;
+    const int chunks = (a.c.heads * a.c.row16 + 31) / 32;
+    const int chunk = blockIdx.y % chunks, mat = (blockIdx.y / chunks) & 1, layer = blockIdx.y / (2 * chunks);
+    const int ctx = __ldg(a.context + s), n = min(max(__ldg(a.n_path + s), 0), a.max_path);
+    if (blockIdx.y == 0 && lane == 0) a.new_context[s] = ctx + n;
+    const long long cap = (long long)a.table_width << a.c.page_shift;
+    const int mask = (1 << a.c.page_shift) - 1;
+    bool any = false;
+    for (int i = lane; i < n; i += 32) {
+        const int node = __ldg(a.path + (long long)s * a.max_path + i);
+        const long long src = (long long)ctx + node, dst = (long long)ctx + i;
+        long long f = -1, t = -1;
+        if (ctx >= 0 && node >= 0 && node != i && src < cap && dst < cap) {
+            const int32_t *table = a.page_table + (long long)s * a.table_width;
+            const int ps = __ldg(table + (src >> a.c.page_shift)), pd = __ldg(table + (dst >> a.c.page_shift));
+            if ((unsigned)ps < (unsigned)a.c.n_pages && (unsigned)pd < (unsigned)a.c.n_pages) {
+                f = kv_row(a.c, layer, ps, 0, (int)(src & mask));
+                t = kv_row(a.c, layer, pd, 0, (int)(dst & mask));
+                any = true;
+            }
+        }
+        from[i] = f;
+        to[i] = t;
+    }
+    if (!__any_sync(0xffffffffu, any)) return;
+    __syncwarp();
+    const int i = chunk * 32 + lane;
+    if (i >= a.c.heads * a.c.row16) return;
+    const long long off = (long long)(i / a.c.row16) * ((long long)a.c.row16 << a.c.page_shift) + i % a.c.row16;
+    uint4 *pool = a.pool[mat] + off;
+    if (n <= 8) {
+        uint4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n && from[j] >= 0) x[j] = pool[from[j] * a.c.row16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n && from[j] >= 0) pool[to[j] * a.c.row16] = x[j];
+    } else {
+#pragma unroll 8
+        for (int j = 0; j < n; ++j)
+            if (from[j] >= 0) rows[j][lane] = pool[from[j] * a.c.row16];
+        for (int j = 0; j < n; ++j)
+            if (from[j] >= 0) pool[to[j] * a.c.row16] = rows[j][lane];
+    }
+}
+
+// blockIdx.x: piece of a page, .y: pair, .z: layer and matrix
+struct KvCopyArgs {
+    uint4 *pool[2];
+    long long page16;                     // 16-byte words of a page
+    int n_pages;
+    int pair[kKvPairs][2];
+};
+constexpr int kKvCopyThreads = 256, kKvCopyWords = kKvCopyThreads * 8;
+__global__ void __launch_bounds__(kKvCopyThreads) kv_copy_kernel(const __grid_constant__ KvCopyArgs a)
+{
+    uint4 *pool = a.pool[blockIdx.z & 1] + (long long)(blockIdx.z >> 1) * a.n_pages * a.page16;
+    const uint4 *src = pool + a.pair[blockIdx.y][0] * a.page16;
+    uint4 *dst = pool + a.pair[blockIdx.y][1] * a.page16;
+    const long long i0 = (long long)blockIdx.x * kKvCopyWords + threadIdx.x;
+    uint4 x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i0 + j * kKvCopyThreads < a.page16) x[j] = __ldcs(src + i0 + j * kKvCopyThreads);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i0 + j * kKvCopyThreads < a.page16) __stcs(dst + i0 + j * kKvCopyThreads, x[j]);
+}
+
+}  // namespace s2moe

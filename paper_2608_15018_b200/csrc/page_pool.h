@@ -1,0 +1,138 @@
+// Who owns which page of a paged key/value cache: host-side bookkeeping only, no CUDA in here.
+//
+// A sequence is a list of pages; page i holds positions i * page_size and up.  A fork shares all pages of its parent
+// (every page counts its owners).  Before positions are written they are reserved: missing pages are taken (lowest
+// free number first), and a page that others own too is replaced by one of the sequence's own; the pair (old, new) says
+// what has to be copied on the device before the write.  Truncating gives pages back.  Compacting moves pages to the
+// lowest numbers and says which copies that takes; no copy's source is another's destination.
+#pragma once
+
+#include <cstdint>
+#include <set>
+#include <utility>
+#include <vector>
+
+namespace s2moe {
+
+struct PagePool {
+    int n_pages = 0, page_size = 0;
+    std::vector<int32_t> owners;                       // page -> sequences that hold it
+    std::set<int32_t> free_pages;
+    std::vector<std::vector<int32_t>> seqs;            // sequence -> pages
+    std::vector<char> alive;
+
+    PagePool(int pages, int size) : n_pages(pages), page_size(size), owners((size_t)pages, 0)
+    {
+        for (int i = 0; i < pages; ++i) free_pages.insert(free_pages.end(), i);
+    }
+    bool known(int s) const { return s >= 0 && s < (int)seqs.size() && alive[(size_t)s]; }
+    int32_t open()
+    {
+        for (size_t i = 0; i < seqs.size(); ++i)
+            if (!alive[i]) {
+                seqs[i].clear();
+                alive[i] = 1;
+                return (int32_t)i;
+            }
+        seqs.reserve(seqs.size() + 1);
+        alive.reserve(alive.size() + 1);
+        seqs.emplace_back();
+        alive.push_back(1);
+        return (int32_t)seqs.size() - 1;
+    }
+    int32_t fork(int s)
+    {
+        std::vector<int32_t> pages = seqs[(size_t)s];
+        const int32_t t = open();
+        for (int32_t p : pages) ++owners[(size_t)p];
+        seqs[(size_t)t].swap(pages);
+        return t;
+    }
+    int32_t take()
+    {
+        const int32_t p = *free_pages.begin();
+        free_pages.erase(free_pages.begin());
+        owners[(size_t)p] = 1;
+        return p;
+    }
+    void release(int32_t p)
+    {
+        if (--owners[(size_t)p] == 0) free_pages.insert(p);
+    }
+    // pairs that reserve() names
+    int32_t copies_needed(int s, int64_t from, int64_t to) const
+    {
+        const std::vector<int32_t> &pages = seqs[(size_t)s];
+        int32_t n = 0;
+        for (int64_t i = from / page_size; i < (int64_t)pages.size() && i * page_size < to && from < to; ++i)
+            n += owners[(size_t)pages[(size_t)i]] > 1 && (i * page_size < from || (i + 1) * page_size > to);
+        return n;
+    }
+    // pairs that compact() names
+    int32_t moves_needed() const
+    {
+        const int32_t used = n_pages - (int32_t)free_pages.size();
+        int32_t n = 0;
+        for (int32_t p = used; p < n_pages; ++p) n += owners[(size_t)p] > 0;
+        return n;
+    }
+    // Pages for positions [from, to) that the sequence alone owns.  False, changing nothing, when the pool has not
+    // enough free pages.
+    bool reserve(int s, int64_t from, int64_t to, std::vector<std::pair<int32_t, int32_t>> &copies)
+    {
+        std::vector<int32_t> &pages = seqs[(size_t)s];
+        const int64_t have = (int64_t)pages.size(), need = (to + page_size - 1) / page_size;
+        const int64_t lo = from / page_size, hi = need < have ? need : have;
+        int64_t take_n = need > have ? need - have : 0;
+        for (int64_t i = lo; i < hi && from < to; ++i)
+            if (owners[(size_t)pages[(size_t)i]] > 1) ++take_n;
+        if (take_n > (int64_t)free_pages.size()) return false;
+        copies.reserve((size_t)take_n);
+        if (need > have) pages.reserve((size_t)need);
+        for (int64_t i = lo; i < hi && from < to; ++i) {
+            const int32_t old = pages[(size_t)i];
+            if (owners[(size_t)old] <= 1) continue;
+            const int32_t p = take();
+            // positions of the page outside [from, to) are still needed
+            if (i * page_size < from || (i + 1) * page_size > to) copies.emplace_back(old, p);
+            --owners[(size_t)old];
+            pages[(size_t)i] = p;
+        }
+        while ((int64_t)pages.size() < need) pages.push_back(take());
+        return true;
+    }
+    void truncate(int s, int64_t length)
+    {
+        std::vector<int32_t> &pages = seqs[(size_t)s];
+        const int64_t keep = (length + page_size - 1) / page_size;
+        while ((int64_t)pages.size() > keep) {
+            release(pages.back());
+            pages.pop_back();
+        }
+    }
+    void close(int s)
+    {
+        truncate(s, 0);
+        alive[(size_t)s] = 0;
+    }
+    void compact(std::vector<std::pair<int32_t, int32_t>> &copies)
+    {
+        const int32_t used = n_pages - (int32_t)free_pages.size();
+        std::vector<int32_t> now((size_t)n_pages);
+        for (int32_t i = 0; i < n_pages; ++i) now[(size_t)i] = i;
+        for (int32_t p = n_pages - 1; p >= used; --p) {
+            if (owners[(size_t)p] == 0) continue;
+            const int32_t q = *free_pages.begin();       // below `used`: as many are free there as are taken above
+            free_pages.erase(free_pages.begin());
+            free_pages.insert(p);
+            owners[(size_t)q] = owners[(size_t)p];
+            owners[(size_t)p] = 0;
+            now[(size_t)p] = q;
+            copies.emplace_back(p, q);
+        }
+        for (auto &pages : seqs)
+            for (auto &p : pages) p = now[(size_t)p];
+    }
+};
+
+}  // namespace s2moe

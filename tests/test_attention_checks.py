@@ -1,0 +1,183 @@
+"""Refusals of the attention and cache calls: all of them answer before anything reaches the device (CPU only)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2608_15018_b200 import binding
+
+P = 1 << 20                                                     # an address that is never followed
+
+
+def cache(**change):
+    f = dict(k=P, v=P, dtype=binding.BF16, n_layers=2, n_pages=8, n_kv_heads=4, page_size=16, head_dim=64)
+    f.update(change)
+    return binding.KVCacheC(*f.values())
+
+
+BAD_CACHES = [dict(k=None), dict(v=None), dict(k=P + 8), dict(dtype=2), dict(dtype=-1), dict(n_layers=0), dict(n_pages=0),
+              dict(n_kv_heads=0), dict(page_size=48), dict(page_size=8), dict(page_size=256), dict(head_dim=96), dict(head_dim=256)]
+
+
+def prompt(**change):
+    f = dict(dtype=binding.BF16, n_seq=2, n_tokens=10, n_heads=8, n_kv_heads=4, head_dim=64, q=P, q_stride=512, k=P, k_stride=256, v=P,
+             v_stride=256, seq_start=P, scale=0.125, out=P, stream=None)
+    f.update(change)
+    return binding.load_library().s2moe_prompt_attention(*f.values())
+
+
+@pytest.mark.parametrize("change", [
+    dict(dtype=2), dict(n_seq=-1), dict(n_tokens=-1), dict(n_heads=9), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=512, q_stride=1 << 16),
+    dict(head_dim=32), dict(head_dim=80), dict(q=None), dict(k=None), dict(v=None), dict(seq_start=None), dict(out=None), dict(q=P + 2),
+    dict(k=P + 8), dict(v=P + 4), dict(out=P + 8), dict(q_stride=511), dict(q_stride=508), dict(k_stride=248), dict(v_stride=252),
+    dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))])
+def test_prompt_attention_refuses(change):
+    assert prompt(**change) == binding.EINVAL
+
+
+def test_prompt_attention_sizes():
+    assert prompt(n_tokens=2 ** 29) == binding.ERANGE
+    assert prompt(n_tokens=0) == binding.OK and prompt(n_seq=0) == binding.OK
+
+
+def tree(c=None, **change):
+    f = dict(layer=1, n_seq=2, n_tokens=10, n_heads=8, q=P, q_stride=512, page_table=P, table_width=4, context=P, seq_start=P, n_nodes=10,
+             node_start=None, parent=P, scale=0.125, out=P, workspace=P, workspace_bytes=1 << 40, stream=None)
+    f.update(change)
+    return binding.load_library().s2moe_tree_attention(None if c is None else ctypes.byref(c), *f.values())
+
+
+@pytest.mark.parametrize("change", BAD_CACHES)
+def test_every_call_refuses_a_bad_cache(change):
+    lib, c = binding.load_library(), cache(**change)
+    n = ctypes.c_int64(5)
+    assert tree(c) == binding.EINVAL
+    assert lib.s2moe_tree_attention_workspace(ctypes.byref(c), 2, 10, 8, 4, ctypes.byref(n)) == binding.EINVAL and n.value == 0
+    assert lib.s2moe_kv_write(ctypes.byref(c), 0, 2, 10, P, 512, P, 512, P, 4, P, P, None) == binding.EINVAL
+    assert lib.s2moe_kv_commit(ctypes.byref(c), 2, P, 4, P, P, 4, P, P + 64, None) == binding.EINVAL
+    assert lib.s2moe_kv_copy_pages(ctypes.byref(c), 1, (ctypes.c_int32 * 2)(0, 1), None) == binding.EINVAL
+
+
+@pytest.mark.parametrize("change", [
+    dict(n_seq=-1), dict(n_tokens=-1), dict(n_nodes=-1), dict(n_nodes=9), dict(table_width=0), dict(n_heads=6), dict(n_heads=1024),
+    dict(q=None), dict(page_table=None), dict(context=None), dict(seq_start=None), dict(out=None), dict(q=P + 2), dict(out=P + 8),
+    dict(q_stride=256), dict(q_stride=516), dict(scale=-0.5), dict(scale=float("nan"))])
+def test_tree_attention_refuses(change):
+    assert tree(cache(), **change) == binding.EINVAL
+
+
+def test_tree_attention_sizes():
+    assert tree(None) == binding.EINVAL
+    assert tree(cache(), layer=2) == binding.ERANGE and tree(cache(), layer=-1) == binding.ERANGE
+    assert tree(cache(), n_tokens=2 ** 29, n_nodes=2 ** 29) == binding.ERANGE
+    assert tree(cache(), table_width=2 ** 27) == binding.ERANGE
+    assert tree(cache(n_pages=2 ** 26)) == binding.ERANGE
+    assert tree(cache(), n_tokens=0, n_nodes=0) == binding.OK and tree(cache(), n_seq=0) == binding.OK
+    assert binding.load_library().s2moe_attention_status(None) == binding.EINVAL
+
+
+def test_kv_write_refuses():
+    lib, c = binding.load_library(), cache()
+    good = dict(layer=0, n_seq=2, n_tokens=10, k=P, k_stride=256, v=P, v_stride=256, page_table=P, table_width=4, first=P, seq_start=P, stream=None)
+    call = lambda **f: lib.s2moe_kv_write(ctypes.byref(c), *{**good, **f}.values())
+    for f in (dict(n_seq=-1), dict(n_tokens=-1), dict(table_width=0), dict(k=None), dict(v=None), dict(page_table=None), dict(first=None),
+              dict(seq_start=None), dict(k=P + 2), dict(v=P + 8), dict(k_stride=128), dict(v_stride=260)):
+        assert call(**f) == binding.EINVAL, f
+    assert call(layer=2) == binding.ERANGE and call(layer=-1) == binding.ERANGE
+    assert call(n_tokens=0) == binding.OK and call(n_seq=0) == binding.OK
+
+
+def test_kv_commit_refuses():
+    lib, c = binding.load_library(), cache()
+    good = dict(n_seq=2, page_table=P, table_width=4, context=P, path=P, max_path=4, n_path=P, new_context=P + 64, stream=None)
+    call = lambda cc=c, **f: lib.s2moe_kv_commit(ctypes.byref(cc), *{**good, **f}.values())
+    for f in (dict(n_seq=-1), dict(table_width=0), dict(max_path=0), dict(page_table=None), dict(context=None), dict(path=None),
+              dict(n_path=None), dict(new_context=None), dict(new_context=P), dict(new_context=P + 4)):
+        assert call(**f) == binding.EINVAL, f
+    assert call(max_path=65) == binding.ERANGE
+    assert call(cache(n_layers=32768)) == binding.ERANGE
+    assert call(n_seq=0) == binding.OK
+
+
+def test_kv_copy_pages_refuses():
+    lib, c = binding.load_library(), cache()
+    call = lambda *pages: lib.s2moe_kv_copy_pages(ctypes.byref(c), len(pages) // 2, (ctypes.c_int32 * len(pages))(*pages), None)
+    assert call(0, 8) == binding.ERANGE and call(-1, 2) == binding.ERANGE and call(8, 2) == binding.ERANGE and call(2, -1) == binding.ERANGE
+    for pages in ((3, 3), (0, 1, 2, 1), (0, 1, 1, 2), (1, 2, 0, 1), (0, 1, 2, 0)):
+        assert call(*pages) == binding.EINVAL, pages
+    assert lib.s2moe_kv_copy_pages(ctypes.byref(c), 1, None, None) == binding.EINVAL
+    assert lib.s2moe_kv_copy_pages(ctypes.byref(c), -1, None, None) == binding.EINVAL
+    assert lib.s2moe_kv_copy_pages(ctypes.byref(c), 0, None, None) == binding.OK
+
+
+class _Library:
+    """Records the calls that would have reached the device."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return binding.OK
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = _Library()
+    monkeypatch.setattr(binding, "load_library", lambda: lib)
+    monkeypatch.setattr(binding, "_on_device", lambda device, **tensors: None)
+    monkeypatch.setattr(binding, "_dptr", lambda t: t.data_ptr())
+    monkeypatch.setattr(binding, "_stream_handle", lambda stream: 0)
+    return lib
+
+
+def i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def test_python_calls_refuse_wrong_shapes_and_types(library):
+    bf = dict(dtype=torch.bfloat16)
+    q, k = torch.zeros(5, 8, 64, **bf), torch.zeros(5, 4, 64, **bf)
+    for args in ((q.half(), k.half(), k.half(), i32(3)), (q, k[:4], k, i32(3)), (q, k, k.float(), i32(3)), (q, k, k, i32(3).long()),
+                 (q, k, k, i32(3, 1)), (q.transpose(0, 1), k, k, i32(3)), (q[:, :, ::2], k[:, :, ::2], k[:, :, ::2], i32(3)),
+                 (q, torch.zeros(5, 4, 32, **bf), torch.zeros(5, 4, 32, **bf), i32(3)), (q[0], k, k, i32(3)), (q, k, k, i32(0))):
+        with pytest.raises((ValueError, TypeError)):
+            binding.prompt_attention(*args)
+    for out in (torch.zeros(5, 8, 64), torch.zeros(4, 8, 64, **bf), torch.zeros(5, 8, 128, **bf)[:, :, :64]):
+        with pytest.raises(ValueError, match="out"):
+            binding.prompt_attention(q, k, k, i32(3), out=out)
+    for pool in ((torch.zeros(2, 8, 4, 16, 64), torch.zeros(2, 8, 4, 16, 64, **bf)), (torch.zeros(8, 4, 16, 64),) * 2,
+                 (torch.zeros(2, 8, 4, 16, 64).half(),) * 2):
+        with pytest.raises(ValueError):
+            binding.KVCache(*pool)
+    c = binding.KVCache(torch.zeros(2, 8, 4, 16, 64, **bf), torch.zeros(2, 8, 4, 16, 64, **bf))
+    good = dict(q=q, cache=c, layer=0, page_table=i32(2, 3), context=i32(2), seq_start=i32(3), parent=i32(5), node_start=None)
+    for f in (dict(q=q.float()), dict(page_table=i32(3, 3)), dict(page_table=i32(6)), dict(context=i32(3)), dict(seq_start=i32(3).long()),
+              dict(parent=i32(4)), dict(parent=i32(5).long()), dict(node_start=i32(2), parent=i32(9)), dict(node_start=i32(3), parent=None),
+              dict(page_table=i32(2, 6)[:, ::2]), dict(q=torch.zeros(5, 8, 128, **bf))):
+        with pytest.raises(ValueError):
+            binding.tree_attention(**{**good, **f})
+    kk = torch.zeros(5, 4, 64, **bf)
+    for f in (dict(k=kk[:4]), dict(k=kk.float(), v=kk.float()), dict(first=i32(1)), dict(page_table=i32(1, 3)), dict(seq_start=i32(2, 2))):
+        with pytest.raises(ValueError):
+            binding.kv_write(**{**dict(cache=c, layer=0, k=kk, v=kk, page_table=i32(2, 3), first=i32(2), seq_start=i32(3)), **f})
+    for f in (dict(context=i32(3)), dict(path=i32(2)), dict(path=i32(3, 4)), dict(n_path=i32(2, 1)), dict(out=i32(3)), dict(out=i32(2).long())):
+        with pytest.raises(ValueError):
+            binding.kv_commit(**{**dict(cache=c, page_table=i32(2, 3), context=i32(2), path=i32(2, 4), n_path=i32(2)), **f})
+    assert not library.calls
+    wide = torch.zeros(5, 16 * 64, **bf)                         # parts of one projection's output are taken as they are
+    binding.prompt_attention(wide[:, :512].unflatten(1, (8, 64)), wide[:, 512:768].unflatten(1, (4, 64)), wide[:, 768:].unflatten(1, (4, 64)), i32(3))
+    args = library.calls[-1][1]
+    assert args[7] == args[9] == args[11] == 1024 and args[8] - args[6] == 1024 and args[10] - args[6] == 1536
+
+
+def test_tensors_on_another_device_than_the_current_one(monkeypatch):
+    monkeypatch.setattr(binding, "_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        binding._on_device(torch.device("cuda", 0))
+    with pytest.raises(ValueError, match="cpu"):
+        binding._on_device(torch.device("cpu"))
+    with pytest.raises(ValueError, match="x is on"):
+        binding._on_device(torch.device("cuda", 1), x=i32(2))
