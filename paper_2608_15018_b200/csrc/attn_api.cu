@@ -4,11 +4,13 @@
 
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <new>
 #include <vector>
 
 #include "attn_common.cuh"
 #include "attn_simple.cuh"
+#include "attn_tc.cuh"
 #include "kv_cache.cuh"
 #include "page_pool.h"
 
@@ -22,6 +24,8 @@ struct s2moe_pages {
 namespace {
 
 __device__ int g_attn_status;
+
+constexpr int64_t kMaxRows = 1 << 30;      // rows (token, query head) of a call
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 int elem_size(int dtype) { return dtype == S2MOE_F32 ? 4 : 2; }
@@ -70,26 +74,65 @@ int launch_status() { return cudaGetLastError() == cudaSuccess ? S2MOE_OK : S2MO
 // workspace query.
 struct TreePlan {
     int rows_tile, grid, min_units, key_tile;
-    bool split;
+    bool split, pair;
     int64_t items;                 // upper bound
     int64_t workspace;
 };
 
-TreePlan tree_plan(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_heads, int head_dim, int64_t capacity, int n_sm)
+// rows of a 128-row block that are in use: whole tokens
+int tc_rows(int group) { return kAttnTile / group * group; }
+
+TreePlan tree_plan(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_heads, int64_t capacity, int head_dim, int n_sm)
 {
     TreePlan p{};
     const int group = n_heads / n_kv_heads;
-    (void)dtype;
-    // rows of one sequence at most: trees with parents have up to 64 tokens, chains any number
     const int64_t rows = (int64_t)n_tokens * group;
-    p.rows_tile = rows <= 16 ? 16 : 64;
-    p.key_tile = kAttnSimpleTile;
-    p.min_units = 4;
+    if (dtype == S2MOE_F32) {
+        p.rows_tile = rows <= 16 * (int64_t)n_seq ? 16 : 64;
+        p.key_tile = kAttnSimpleTile;
+        p.min_units = 4;
+        p.grid = 2 * n_sm;
+    } else {
+        p.pair = rows > (int64_t)n_seq * tc_rows(group);
+        p.rows_tile = tc_rows(group) * (p.pair ? 2 : 1);
+        p.key_tile = kAttnTile;
+        p.min_units = 2;
+        p.grid = n_sm;
+    }
     p.items = (int64_t)n_kv_heads * (rows / p.rows_tile + (n_tokens < n_seq ? n_tokens : n_seq));
     p.split = capacity > (int64_t)p.min_units * p.key_tile;
-    p.grid = 2 * n_sm;
     p.workspace = p.split ? (int64_t)p.grid * 2 * p.rows_tile * (head_dim + 2) * 4 : 0;
     return p;
+}
+
+// ---- tensor maps ----------------------------------------------------------------------------------------------------
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static std::atomic<void *> known{nullptr};             // the driver's entry point, the same for the whole process
+    void *fn = known.load(std::memory_order_relaxed);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult res;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess ||
+            res != cudaDriverEntryPointSuccess)
+            return nullptr;
+        known.store(fn, std::memory_order_relaxed);
+    }
+    return (EncodeTiled)fn;
+}
+
+// bfloat16 [n2][n1][n0] with strides in elements, boxes of 64 x b1 x b2, 128-byte swizzle
+bool make_map(CUtensorMap *m, const void *base, int64_t n0, int64_t n1, int64_t n2, int64_t s1, int64_t s2, int b1, int b2)
+{
+    EncodeTiled fn = encode_tiled();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)n0, (cuuint64_t)n1, (cuuint64_t)n2}, strides[2] = {(cuuint64_t)s1 * 2, (cuuint64_t)s2 * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)b1, (cuuint32_t)b2}, one[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename K, typename... A>
@@ -110,33 +153,61 @@ int launch(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, b
     return cudaLaunchKernelEx(&lc, kernel, args...) == cudaSuccess ? S2MOE_OK : S2MOE_ECUDA;
 }
 
-template <typename T, int D, int R, bool PAGED, bool SPLIT>
+int64_t grid_for(int64_t items) { return items < (1 << 20) ? items : 1 << 20; }
+
+template <int D, int R, bool PAGED, bool SPLIT>
 int launch_simple(const AttnArgs &a, int64_t grid, cudaStream_t st)
 {
-    return launch(attn_simple_kernel<T, D, R, PAGED, SPLIT>, grid, kAttnSimpleThreads, (size_t)attn_simple_smem(D, R), st, false, a);
+    return launch(attn_simple_kernel<float, D, R, PAGED, SPLIT>, grid, kAttnSimpleThreads, (size_t)attn_simple_smem(D, R), st, false, a);
 }
 
-template <typename T, int D>
-int run_prompt(AttnArgs a, cudaStream_t st)
+template <int D, bool PAGED, bool PAIR, bool SPLIT>
+int launch_tc(const AttnMaps &maps, const AttnArgs &a, int64_t grid, cudaStream_t st)
 {
-    a.rows_tile = 64;
-    int64_t items = (int64_t)a.Hk * ((int64_t)a.n_tokens * a.group / 64 + a.n_seq);
-    if (items > (1 << 20)) items = 1 << 20;
-    return launch_simple<T, D, 64, false, false>(a, items, st);
+    return launch(attn_tc_kernel<D, PAGED, PAIR, SPLIT>, grid, kAttnThreads, (size_t)AttnSmem<D, PAIR>::bytes, st, false, maps, a);
 }
 
-template <typename T, int D>
-int run_tree(AttnArgs a, const TreePlan &p, cudaStream_t st)
+template <int D>
+int run_prompt(int dtype, AttnArgs a, cudaStream_t st)
+{
+    const int64_t rows = (int64_t)a.n_tokens * a.group;
+    if (dtype == S2MOE_F32) {
+        a.rows_tile = 64;
+        return launch_simple<D, 64, false, false>(a, grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq)), st);
+    }
+    a.rows_tile = 2 * tc_rows(a.group);
+    AttnMaps maps;
+    if (!make_map(&maps.q, a.q, D, (int64_t)a.Hk * a.group, a.n_tokens, D, a.q_stride, a.group, kAttnTile / a.group) ||
+        !make_map(&maps.k, a.k, D, a.Hk, a.n_tokens, D, a.k_stride, 1, kAttnTile) ||
+        !make_map(&maps.v, a.v, D, a.Hk, a.n_tokens, D, a.v_stride, 1, kAttnTile))
+        return S2MOE_ECUDA;
+    return launch_tc<D, false, true, false>(maps, a, grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq)), st);
+}
+
+template <int D>
+int run_tree(int dtype, AttnArgs a, const TreePlan &p, cudaStream_t st)
 {
     a.rows_tile = p.rows_tile;
     a.min_units = p.min_units;
-    if (!p.split) {
-        const int64_t items = p.items < (1 << 20) ? p.items : 1 << 20;
-        return p.rows_tile == 16 ? launch_simple<T, D, 16, true, false>(a, items, st) : launch_simple<T, D, 64, true, false>(a, items, st);
+    const int64_t grid = p.split ? p.grid : grid_for(p.items), join = ((int64_t)a.n_tokens * a.Hk + 3) / 4;
+    int rc;
+    if (dtype == S2MOE_F32) {
+        if (p.rows_tile == 16) rc = p.split ? launch_simple<D, 16, true, true>(a, grid, st) : launch_simple<D, 16, true, false>(a, grid, st);
+        else rc = p.split ? launch_simple<D, 64, true, true>(a, grid, st) : launch_simple<D, 64, true, false>(a, grid, st);
+        if (rc != S2MOE_OK || !p.split) return rc;
+        return launch(attn_join_kernel<float, D, kAttnSimpleTile>, join, 128, 0, st, true, a, p.grid);
     }
-    const int rc = p.rows_tile == 16 ? launch_simple<T, D, 16, true, true>(a, p.grid, st) : launch_simple<T, D, 64, true, true>(a, p.grid, st);
-    if (rc != S2MOE_OK) return rc;
-    return launch(attn_join_kernel<T, D, kAttnSimpleTile>, ((int64_t)a.n_tokens * a.Hk + 3) / 4, 128, 0, st, true, a, p.grid);
+    const int page = 1 << a.page_shift;
+    const int64_t rows = (int64_t)a.n_pages * a.Hk;
+    AttnMaps maps;
+    if (!make_map(&maps.q, a.q, D, (int64_t)a.Hk * a.group, a.n_tokens, D, a.q_stride, a.group, kAttnTile / a.group) ||
+        !make_map(&maps.k, a.k, D, page, rows, D, (int64_t)page * D, page, 1) ||
+        !make_map(&maps.v, a.v, D, page, rows, D, (int64_t)page * D, page, 1))
+        return S2MOE_ECUDA;
+    if (p.pair) rc = p.split ? launch_tc<D, true, true, true>(maps, a, grid, st) : launch_tc<D, true, true, false>(maps, a, grid, st);
+    else rc = p.split ? launch_tc<D, true, false, true>(maps, a, grid, st) : launch_tc<D, true, false, false>(maps, a, grid, st);
+    if (rc != S2MOE_OK || !p.split) return rc;
+    return launch(attn_join_kernel<__nv_bfloat16, D, kAttnTile>, join, 128, 0, st, true, a, p.grid);
 }
 
 }  // namespace
@@ -157,7 +228,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     if (q_stride % per16 || k_stride % per16 || v_stride % per16) return S2MOE_EINVAL;
     if (q_stride < (int64_t)n_heads * head_dim || k_stride < (int64_t)n_kv_heads * head_dim || v_stride < (int64_t)n_kv_heads * head_dim)
         return S2MOE_EINVAL;
-    if ((int64_t)n_tokens * n_heads > INT32_MAX) return S2MOE_ERANGE;
+    if ((int64_t)n_tokens * n_heads > kMaxRows) return S2MOE_ERANGE;
     AttnArgs a{};
     a.q = q; a.k = k; a.v = v; a.out = out;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
@@ -168,8 +239,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     a.status = status_word();
     if (!a.status) return S2MOE_ECUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == S2MOE_F32) return head_dim == 64 ? run_prompt<float, 64>(a, st) : run_prompt<float, 128>(a, st);
-    return head_dim == 64 ? run_prompt<__nv_bfloat16, 64>(a, st) : run_prompt<__nv_bfloat16, 128>(a, st);
+    return head_dim == 64 ? run_prompt<64>(dtype, a, st) : run_prompt<128>(dtype, a, st);
 }
 
 int s2moe_tree_attention_workspace(const s2moe_kv_cache *cache, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t table_width,
@@ -183,8 +253,8 @@ int s2moe_tree_attention_workspace(const s2moe_kv_cache *cache, int32_t n_seq, i
     if (n_seq == 0 || n_tokens == 0) return S2MOE_OK;
     const int n_sm = sm_count();
     if (n_sm < 1) return S2MOE_ECUDA;
-    *bytes = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads, cache->head_dim, (int64_t)table_width * cache->page_size,
-                       n_sm).workspace;
+    *bytes = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads, (int64_t)table_width * cache->page_size,
+                       cache->head_dim, n_sm).workspace;
     return S2MOE_OK;
 }
 
@@ -203,11 +273,11 @@ int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_s
     if (!q || !page_table || !context || !seq_start || !out) return S2MOE_EINVAL;
     if (!aligned16(q) || !aligned16(out) || q_stride % (16 / elem_size(cache->dtype)) || q_stride < (int64_t)n_heads * cache->head_dim)
         return S2MOE_EINVAL;
-    if ((int64_t)n_tokens * n_heads > INT32_MAX || (int64_t)table_width * cache->page_size > INT32_MAX - 128) return S2MOE_ERANGE;
+    if ((int64_t)n_tokens * n_heads > kMaxRows || (int64_t)table_width * cache->page_size > INT32_MAX - 128) return S2MOE_ERANGE;
     const int n_sm = sm_count();
     if (n_sm < 1) return S2MOE_ECUDA;
-    const TreePlan p = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads, cache->head_dim,
-                                 (int64_t)table_width * cache->page_size, n_sm);
+    const TreePlan p = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads,
+                                 (int64_t)table_width * cache->page_size, cache->head_dim, n_sm);
     if (p.workspace > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < p.workspace)) return S2MOE_EINVAL;
     const int64_t layer_bytes = (int64_t)cache->n_pages * cache->n_kv_heads * cache->page_size * cache->head_dim * elem_size(cache->dtype);
     AttnArgs a{};
@@ -226,9 +296,7 @@ int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_s
     a.status = status_word();
     if (!a.status) return S2MOE_ECUDA;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const bool wide = cache->head_dim == 128;
-    if (cache->dtype == S2MOE_F32) return wide ? run_tree<float, 128>(a, p, st) : run_tree<float, 64>(a, p, st);
-    return wide ? run_tree<__nv_bfloat16, 128>(a, p, st) : run_tree<__nv_bfloat16, 64>(a, p, st);
+    return cache->head_dim == 64 ? run_tree<64>(cache->dtype, a, p, st) : run_tree<128>(cache->dtype, a, p, st);
 }
 
 int s2moe_attention_status(int32_t *host_out)

@@ -1,4 +1,4 @@
-// Attention on the CUDA cores, for every type (binary32 runs on it), and the kernel that joins the pieces of split items.
+// Attention on the CUDA cores, for binary32, and the kernel that joins the pieces of split items.
 //
 // A CTA of 256 threads holds R rows of q and takes the keys 64 at a time: scores by register tiles of R/16 rows x 4
 // keys per thread, the running maximum m and sum l of the softmax (p = 2^(s - m), l' = l 2^(m - m') + sum p, likewise
@@ -36,10 +36,11 @@ __device__ __forceinline__ void attn_store4(__nv_bfloat16 *p, float4 v)
     *reinterpret_cast<uint2 *>(p) = make_uint2(reinterpret_cast<uint32_t &>(lo), reinterpret_cast<uint32_t &>(hi));
 }
 
-// The rows of `again` lanes (bit per lane) once more, one by one by the whole warp; each lane names its own row.
+// The rows of `again` lanes (bit per lane) once more, one by one by the whole warp; each lane names its own row.  Columns
+// c0 to c1 - 1 are written.
 template <typename T, int D, bool PAGED>
 __device__ __forceinline__ void attn_fix_rows(const AttnArgs &a, const AttnSeq &q, int s, int h, unsigned again, int token, int head,
-                                              int kend, bool no_weight)
+                                              int kend, bool no_weight, int c0, int c1)
 {
     const int lane = threadIdx.x & 31;
     while (again) {
@@ -51,7 +52,8 @@ __device__ __forceinline__ void attn_fix_rows(const AttnArgs &a, const AttnSeq &
         if (attn_row_again<T, D, PAGED>(a, q, s, h, tk, hd, kend, nw, o)) {
             T *dst = reinterpret_cast<T *>(a.out) + ((long long)(q.tok0 + tk) * a.Hk * a.group + hd) * D;
 #pragma unroll
-            for (int i = 0; i < D / 32; ++i) dst[lane + 32 * i] = (T)o[i];
+            for (int i = 0; i < D / 32; ++i)
+                if (lane + 32 * i >= c0 && lane + 32 * i < c1) dst[lane + 32 * i] = (T)o[i];
         }
         __syncwarp();
     }
@@ -220,7 +222,7 @@ __global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(Attn
             const unsigned again = (bad & 0xffffu ? 1u : 0u) | (bad >> 16 ? 1u << 16 : 0u);
             if (again) {
                 __syncwarp();
-                attn_fix_rows<T, D, PAGED>(a, q, p.s, p.h, again, token, head, p.t1 * 64, l[i] == 0.f);
+                attn_fix_rows<T, D, PAGED>(a, q, p.s, p.h, again, token, head, p.t1 * 64, l[i] == 0.f, 0, D);
             }
         }
     }

@@ -1,0 +1,486 @@
+// bfloat16 attention on the 5th-generation tensor cores: prompts and draft trees, one kernel.
+//
+// A CTA works on blocks of 128 rows (rows: (token, query head of the group) pairs, see attn_common.cuh) and tiles of 128
+// keys.  S = Q K^T comes from shared memory into tensor memory (128 lanes, one per row, x 128 columns), a softmax thread
+// per row takes it from there, writes the weights P as bfloat16 over it, and O += P V takes P from tensor memory and V
+// from shared memory (V is stored keys x D, so it is the operand whose other dimension is contiguous).  O stays in tensor
+// memory for the whole item.  The running maximum is only moved when a row's maximum grows by more than 2^8: until then
+// weights are at most 2^8, and O need not be read and scaled.
+//
+// Roles: two groups of four softmax warps, one warp that issues the matrix instructions, one that issues the copies.
+// While one group is between its S and its P the tensor cores work for the other one:
+//   PAIR    the two groups hold 128 rows each of the same key/value head and share every tile (many rows)
+//   !PAIR   the two groups hold the same rows and take every other tile, their results are joined at the end (few rows:
+//           the time is that of reading the cache, and two tiles are under way at any time)
+// K and V tiles (32 KB each at D = 128) come through a ring by TMA with the 128-byte swizzle.  Pages of a cache are one copy
+// each per 64 columns; a page that is not there, or lies behind the last key, is a copy from outside the tensor, which
+// fills zeros and reads nothing.
+//
+// Rounding: S, the softmax statistics, P before the product and O are binary32; P enters the product as bfloat16
+// (half a step, 2^-8 relative per weight, as the tensor cores need 16-bit operands), sums are taken before that rounding.
+#pragma once
+
+#include "attn_common.cuh"
+#include "attn_simple.cuh"
+#include "ptx.cuh"
+
+namespace s2moe {
+
+constexpr int kAttnTile = 128;
+constexpr int kAttnThreads = 384;                 // 8 softmax warps, matrix instructions, copies, two warps without work
+constexpr int kAttnHalf = 128 * 128;              // bytes of 128 rows x 64 columns
+constexpr float kAttnSlack = 8.f;                 // log2 of the largest weight before the maximum is moved
+
+template <int D, bool PAIR>
+struct AttnSmem {
+    static constexpr int tile = kAttnHalf * (D / 64);
+    static constexpr int q = tile * (PAIR ? 2 : 1);
+    static constexpr int slots = D == 128 ? 5 : 8;
+    static constexpr int bytes = q + slots * tile + 1024;       // + alignment to the swizzle's 1024 bytes
+};
+
+struct AttnMaps {
+    CUtensorMap q, k, v;
+};
+
+__device__ __forceinline__ void attn_ld32(uint32_t taddr, float *v)
+{
+    uint32_t *r = reinterpret_cast<uint32_t *>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+          "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+          "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+// waits for the loads of v; naming the values keeps their uses behind the wait
+template <int N>
+__device__ __forceinline__ void attn_ld_wait(float (&v)[N])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
+}
+__device__ __forceinline__ void attn_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// bits [0, n) of a word whose bits stand for keys from 32 * j on
+__device__ __forceinline__ uint32_t attn_prefix(int n, int j)
+{
+    n -= 32 * j;
+    return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
+template <int D, bool PAGED, bool PAIR, bool SPLIT>
+__global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_constant__ AttnMaps maps, const AttnArgs a)
+{
+    using L = AttnSmem<D, PAIR>;
+    using Iter = AttnIter<PAGED, SPLIT, kAttnTile>;
+    constexpr int NS = L::slots;
+    extern __shared__ uint8_t attn_raw[];
+    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], p_full[2], ended;
+    __shared__ uint32_t tmem_at;
+    __shared__ float2 ml[2][128];
+    uint8_t *qs = attn_raw + ((1024u - (smem_u32(attn_raw) & 1023u)) & 1023u), *ring = qs + L::q;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int half = PAIR ? a.rows_tile / 2 : a.rows_tile;        // rows of a block that are in use
+    if (SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        mbar_init(&q_full, 1);
+        mbar_init(&q_empty, 1);
+        mbar_init(&ended, 1);
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(&s_full[w], 1);
+            mbar_init(&p_full[w], 4);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_at)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        tc_fence_before();
+    }
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at, tmem_s[2] = {tmem, tmem + 128}, tmem_o[2] = {tmem + 256, tmem + 256 + D};
+    bool ok = true;                                               // false: a bounded wait gave up, run out without waiting
+    auto wait = [&](uint64_t *bar, uint32_t parity) {
+        if (ok && !mbar_wait(bar, parity)) {
+            ok = false;
+            atomicExch(a.status, ST_MBAR_TIMEOUT);
+        }
+    };
+    // tiles of each softmax group: PAIR: the first n of the item's, else every other one
+    auto tiles_of = [&](const AttnPiece &p, int w) -> int {
+        const int nt = p.t1 - p.t0;
+        if (!PAIR) return (nt + 1 - w) / 2;
+        const int row = p.rt * a.rows_tile + w * half;
+        if (row >= p.q.n * a.group) return 0;
+        if (PAGED || w == 1) return nt;
+        const int last = min(p.q.n, (row + half) / a.group) - 1;
+        return min(nt, (attn_limit<PAGED>(p.q, last) + kAttnTile - 1) / kAttnTile);
+    };
+    // A softmax thread holds a row of S (128 registers).  The launch gives 384 threads 168 registers each; moved about, 128
+    // threads keep 72 and 256 have 216, which is the same sum.
+    Iter it(a, lane);
+    AttnPiece p;
+    unsigned r0 = 0;                                              // tiles of the pieces before
+
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    it.begin();
+    if (warp == 9) {
+        // ------------------------------------------------------------------ copies
+        unsigned pieces = 0;
+        const int ppt = PAGED ? kAttnTile >> a.page_shift : 1;
+        while (it.next(p) && __all_sync(0xffffffffu, ok)) {
+            const int nw = PAIR && p.rt * a.rows_tile + half < p.q.n * a.group ? 2 : 1;
+            wait(&q_empty, (pieces & 1u) ^ 1u);
+            if (lane == 0) {
+                mbar_expect_tx(&q_full, (uint32_t)(nw * (D / 64) * half * 128));
+                for (int w = 0; w < nw; ++w)
+                    for (int c = 0; c < D / 64; ++c)
+                        tma_load_3d(qs + w * L::tile + c * kAttnHalf, &maps.q, 64 * c, p.h * a.group,
+                                    p.q.tok0 + (p.rt * a.rows_tile + w * half) / a.group, &q_full);
+            }
+            __syncwarp();
+            for (int t = p.t0; t < p.t1 && __all_sync(0xffffffffu, ok); ++t) {
+                int x = 0;                                        // this lane's page, as the tensor's last coordinate
+                if (PAGED && lane < ppt) {
+                    const int at = t * ppt + lane;
+                    x = a.n_pages * a.Hk;
+                    if (at << a.page_shift < p.q.total) {
+                        const int page = __ldg(a.page_table + (long long)p.s * a.table_width + at);
+                        if ((unsigned)page < (unsigned)a.n_pages) x = page * a.Hk + p.h;
+                    }
+                }
+                for (int kv = 0; kv < 2; ++kv) {
+                    const unsigned n = 2 * (r0 + (t - p.t0)) + kv, slot = n % NS;
+                    wait(&empty[slot], ((n / NS) & 1u) ^ 1u);
+                    if (lane == 0) mbar_expect_tx(&full[slot], L::tile);
+                    __syncwarp();
+                    uint8_t *dst = ring + slot * L::tile;
+                    const CUtensorMap *map = kv ? &maps.v : &maps.k;
+                    if (PAGED) {
+                        if (lane < ppt)
+                            for (int c = 0; c < D / 64; ++c)
+                                tma_load_3d(dst + c * kAttnHalf + ((lane * 128) << a.page_shift), map, 64 * c, 0, x, &full[slot]);
+                    } else if (lane < D / 64) {
+                        tma_load_3d(dst + lane * kAttnHalf, map, 64 * lane, p.h, p.q.tok0 + t * kAttnTile, &full[slot]);
+                    }
+                    __syncwarp();
+                }
+            }
+            r0 += p.t1 - p.t0;
+            ++pieces;
+        }
+        // nothing may land in shared memory that is no longer this CTA's
+        if (!ok)
+            for (int i = 0; i < NS; ++i) mbar_wait(&full[i], 0), mbar_wait(&full[i], 1);
+    } else if (warp == 8) {
+        // ------------------------------------------------------------------ matrix instructions
+        const bool leader = tc_elect();
+        // D = F32, A = B = BF16, M = 128; bit 16: B's rows (not its columns) are contiguous
+        const uint32_t idesc_s = tc_idesc(kAttnTile), idesc_o = tc_idesc(D) | (1u << 16);
+        const uint64_t kd = tc_smem_desc(ring), qd = tc_smem_desc(qs);
+        // V: 64-column blocks kAttnHalf apart, groups of 8 keys 1024 bytes apart
+        const uint64_t vd = (kd & ~(0x3fffull << 16)) | ((uint64_t)(kAttnHalf >> 4) << 16);
+        const uint32_t k_hi = (uint32_t)(kd >> 32), v_hi = (uint32_t)(vd >> 32), q_hi = (uint32_t)(qd >> 32);
+        unsigned pieces = 0;
+        uint32_t p_phase[2] = {0, 0};
+        while (it.next(p)) {
+            if (leader && ok) {
+                const int n[2] = {tiles_of(p, 0), tiles_of(p, 1)}, nt = p.t1 - p.t0;
+                auto scores = [&](int w, int t) {                 // S of group w from tile t of the piece
+                    const unsigned c = 2 * (r0 + t), slot = c % NS;
+                    wait(&full[slot], (c / NS) & 1u);
+                    tc_fence_after();
+                    const uint32_t ql = (uint32_t)qd + (PAIR ? w * (L::tile >> 4) : 0), kl = (uint32_t)kd + slot * (L::tile >> 4);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t o = (k / 4) * (kAttnHalf >> 4) + (k % 4) * 2;
+                        tc_mma_bf16_parts(tmem_s[w], ql + o, q_hi, kl + o, k_hi, idesc_s, k > 0);
+                    }
+                };
+                auto product = [&](int w, int t, bool first) {    // O of group w from its weights and tile t
+                    const unsigned c = 2 * (r0 + t) + 1, slot = c % NS;
+                    wait(&full[slot], (c / NS) & 1u);
+                    wait(&p_full[w], p_phase[w]);
+                    p_phase[w] ^= 1u;
+                    tc_fence_after();
+                    const uint32_t vl = (uint32_t)vd + slot * (L::tile >> 4);
+#pragma unroll
+                    for (int k = 0; k < kAttnTile / 16; ++k)
+                        tc_mma_bf16_tmem_a(tmem_o[w], tmem_s[w] + 8 * k, vl + k * 128, v_hi, idesc_o, !first || k > 0);
+                };
+                auto release = [&](int t, int kv) { tc_commit(&empty[(2 * (r0 + t) + kv) % NS]); };
+                wait(&q_full, pieces & 1u);
+                if (PAIR) {
+                    for (int w = 0; w < 2; ++w)
+                        if (n[w] > 0) {
+                            scores(w, 0);
+                            tc_commit(&s_full[w]);
+                        }
+                    release(0, 0);
+                    if (nt == 1) tc_commit(&q_empty);
+                    for (int t = 0; t < nt && ok; ++t) {
+                        for (int w = 0; w < 2; ++w) {
+                            if (t >= n[w]) continue;
+                            const bool last = w == 1 || t >= n[1], last_k = w == 1 || t + 1 >= n[1];
+                            product(w, t, t == 0);
+                            if (last) release(t, 1);
+                            if (t + 1 < n[w]) {
+                                scores(w, t + 1);
+                                if (last_k) release(t + 1, 0);
+                                if (last_k && t + 2 == nt) tc_commit(&q_empty);
+                            }
+                            tc_commit(&s_full[w]);
+                        }
+                    }
+                } else {
+                    for (int w = 0; w < 2 && w < nt; ++w) {
+                        scores(w, w);
+                        release(w, 0);
+                        tc_commit(&s_full[w]);
+                    }
+                    if (nt <= 2) tc_commit(&q_empty);
+                    for (int t = 0; t < nt && ok; ++t) {
+                        const int w = t & 1;
+                        product(w, t, t < 2);
+                        release(t, 1);
+                        if (t + 2 < nt) {
+                            scores(w, t + 2);
+                            release(t + 2, 0);
+                            if (t + 3 == nt) tc_commit(&q_empty);
+                        }
+                        tc_commit(&s_full[w]);
+                    }
+                }
+            }
+            __syncwarp();
+            r0 += p.t1 - p.t0;
+            ++pieces;
+        }
+        if (leader && !ok) {                                      // no instruction outlives the CTA's tensor memory
+            tc_commit(&ended);
+            mbar_wait(&ended, 0);
+        }
+        __syncwarp();
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        it.begin();
+        // ------------------------------------------------------------------ softmax: one thread per row
+        const int w = warp >> 2, row_in = tid & 127;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // this warp's 32 lanes of tensor memory
+        const uint32_t s_at = tmem_s[w] + lanes, o_at = tmem_o[w] + lanes;
+        const int ppt = PAGED ? kAttnTile >> a.page_shift : 0;
+        uint32_t s_phase = 0;
+        while (it.next(p)) {
+            const AttnSeq &q = p.q;
+            const int n = tiles_of(p, w), row = p.rt * a.rows_tile + (PAIR ? w * half : 0) + row_in;
+            const bool mine = row_in < half && row < q.n * a.group, used = __any_sync(0xffffffffu, mine);
+            const int token = mine ? row / a.group : 0, head = p.h * a.group + (mine ? row % a.group : 0);
+            const int lim = mine ? attn_limit<PAGED>(q, token) : q.total;
+            const bool tree = PAGED && a.parent && !q.bad;
+            unsigned long long anc = ~0ull;
+            if (tree && mine && p.t1 * kAttnTile > q.ctx) anc = attn_ancestors(a, q, q.nodes - q.n + token);
+            // keys below this one every row of the warp sees
+            int clear = tree ? min(lim, q.ctx) : lim;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) clear = min(clear, __shfl_xor_sync(0xffffffffu, clear, o));
+            float m = -CUDART_INF_F, l = 0.f;                     // maximum in use (times scale_log2), sum of weights
+            for (int i = 0; i < n; ++i) {
+                const int t = PAIR ? i : 2 * i + w, key0 = (p.t0 + t) * kAttnTile;
+                unsigned there = 0, all = 0;                      // pages of the tile that exist
+                if (PAGED) {
+                    const int at = (p.t0 + t) * ppt + lane;
+                    bool have = false;
+                    if (lane < ppt && at << a.page_shift < q.total)
+                        have = (unsigned)__ldg(a.page_table + (long long)p.s * a.table_width + at) < (unsigned)a.n_pages;
+                    there = __ballot_sync(0xffffffffu, have);
+                    all = (1u << ppt) - 1u;
+                }
+                wait(&s_full[w], s_phase);
+                s_phase ^= 1u;
+                tc_fence_after();
+                if (key0 + kAttnTile > q.total) {
+                    // rows of V behind the last key can hold anything, and 0 * NaN is no 0
+                    const unsigned c = 2 * (r0 + t) + 1, slot = c % NS;
+                    wait(&full[slot], (c / NS) & 1u);
+                    if (key0 + row_in >= q.total) {
+                        uint4 *v = reinterpret_cast<uint4 *>(ring + slot * L::tile + row_in * 128);
+#pragma unroll
+                        for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[c * (kAttnHalf / 16) + j] = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async();
+                }
+                if (!used) {                                      // no row of the warp is in use: its lanes hold what they hold
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[w]);
+                    continue;
+                }
+                float s[kAttnTile];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) attn_ld32(s_at + 32 * c, s + 32 * c);
+                attn_ld_wait(s);
+                float sc = a.scale_log2;
+                if (key0 + kAttnTile > clear || there != all) {
+                    const int to_lim = lim - key0, to_ctx = q.ctx - key0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t see = attn_prefix(to_lim, j);
+                        if (PAGED) {
+                            if (tree) {
+                                const int up = to_ctx - 32 * j;
+                                const uint32_t nodes = up >= 32 || up <= -64 ? 0u : up >= 0 ? (uint32_t)(anc << up) : (uint32_t)(anc >> -up);
+                                see &= attn_prefix(to_ctx, j) | nodes;
+                            }
+                            if (a.page_shift == 4)
+                                see &= ((there >> (2 * j)) & 1u ? 0xffffu : 0u) | ((there >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
+                            else
+                                see &= (there >> ((32 * j) >> a.page_shift)) & 1u ? ~0u : 0u;
+                        }
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) s[32 * j + c] = (see >> c) & 1u ? s[32 * j + c] * sc : -CUDART_INF_F;
+                    }
+                    sc = 1.f;
+                }
+                float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+                for (int c = 0; c < kAttnTile; c += 8)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mx[j] = fmaxf(fmaxf(mx[j], s[c + 2 * j]), s[c + 2 * j + 1]);
+                float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                top = top == -CUDART_INF_F ? top : top * sc;
+                const bool move = top > m + kAttnSlack || (m == -CUDART_INF_F && top > m);
+                if (__any_sync(0xffffffffu, move)) {
+                    const float f = move ? exp2f(m - top) : 1.f;   // m = -inf: 0
+                    if (move) m = top;
+                    l *= f;
+                    if (i > 0) {                                  // the product before this tile has ended: S came behind it
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            float o[32];
+                            attn_ld32(o_at + 32 * c, o);
+                            attn_ld_wait(o);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o[j] *= f;
+                            tc_st16(o_at + 32 * c, reinterpret_cast<uint32_t(&)[16]>(o[0]));
+                            tc_st16(o_at + 32 * c + 16, reinterpret_cast<uint32_t(&)[16]>(o[16]));
+                        }
+                    }
+                }
+                const float base = m == -CUDART_INF_F ? 0.f : m;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const float x = exp2f(fmaf(s[32 * c + 2 * j], sc, -base)), y = exp2f(fmaf(s[32 * c + 2 * j + 1], sc, -base));
+                        sum[j & 3] += x + y;
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+                        pk[j] = reinterpret_cast<const uint32_t &>(b);
+                    }
+                    tc_st16(s_at + 16 * c, pk);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                attn_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[w]);
+            }
+            if (n > 0) {                                          // the last product
+                wait(&s_full[w], s_phase);
+                s_phase ^= 1u;
+                tc_fence_after();
+            }
+            r0 += p.t1 - p.t0;
+            float f[2] = {1.f, 0.f};
+            bool two = false;
+            if (!PAIR) {
+                ml[w][row_in] = make_float2(m, l);
+                tc_fence_before();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                tc_fence_after();
+                const float2 x = ml[0][row_in], y = ml[1][row_in];
+                two = p.t1 - p.t0 > 1;
+                m = fmaxf(x.x, y.x);
+                const float b = m == -CUDART_INF_F ? 0.f : m;
+                f[0] = exp2f(x.x - b);
+                f[1] = exp2f(y.x - b);
+                l = x.y * f[0] + y.y * f[1];
+            }
+            // the columns this thread writes, 32 at a time
+            constexpr int CW = PAIR ? D : D / 2;
+            const int col0 = PAIR ? 0 : w * CW;
+            const bool part = SPLIT && p.slot >= 0;
+            const float inv = part ? 1.f : q.bad ? CUDART_NAN_F : 1.f / l;
+            bool fine = true;
+            if (used) {
+                const long long at = (long long)p.slot * a.rows_tile + (PAIR ? w * half : 0) + row_in;
+                float *dst_p = a.part_o + at * D + col0;
+                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.out) + ((long long)(q.tok0 + token) * a.Hk * a.group + head) * D + col0;
+#pragma unroll
+                for (int c = 0; c < CW / 32; ++c) {
+                    float o[32];
+                    attn_ld32((PAIR ? o_at : tmem_o[0] + lanes) + col0 + 32 * c, o);
+                    if (!PAIR) {
+                        float o1[32];
+                        if (two) attn_ld32(tmem_o[1] + lanes + col0 + 32 * c, o1);
+                        else
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) o1[j] = 0.f;
+                        attn_ld_wait(o);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) asm volatile("" : "+f"(o1[j]));
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = two ? o[j] * f[0] + o1[j] * f[1] : o[j] * f[0];
+                    } else {
+                        attn_ld_wait(o);
+                    }
+                    if (mine && part) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) attn_store4(dst_p + 32 * c + j, make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+                    } else if (mine) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint32_t u[4];
+#pragma unroll
+                            for (int x = 0; x < 4; ++x) {
+                                const float y0 = o[j + 2 * x] * inv, y1 = o[j + 2 * x + 1] * inv;
+                                fine = fine && attn_finite(y0) && attn_finite(y1);
+                                const __nv_bfloat162 b = __floats2bfloat162_rn(y0, y1);
+                                u[x] = reinterpret_cast<const uint32_t &>(b);
+                            }
+                            *reinterpret_cast<uint4 *>(dst + 32 * c + j) = make_uint4(u[0], u[1], u[2], u[3]);
+                        }
+                    }
+                }
+                if (mine && part && (PAIR || w == 0)) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, l);
+            }
+            if (!PAIR) {                                          // both have read O before the next item's products
+                tc_fence_before();
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                tc_fence_after();
+            }
+            const unsigned again = __ballot_sync(0xffffffffu, mine && !part && !q.bad && !fine);
+            if (again)
+                attn_fix_rows<__nv_bfloat16, D, PAGED>(a, q, p.s, p.h, again, token, head, p.t1 * kAttnTile, l == 0.f, col0, col0 + CW);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+}  // namespace s2moe
