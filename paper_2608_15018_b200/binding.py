@@ -5,7 +5,9 @@ There is no CPU fallback; a missing library raises at first use.
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import itertools
 import os
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -517,45 +519,50 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 def _on_device(device: torch.device, **tensors: Optional[torch.Tensor]) -> None:
     """Every tensor on the current device, the one the kernels are launched on."""
-    if device.type != "cuda" or device.index != _device():
-        raise ValueError(f"tensors on {device}, but the current device is cuda:{_device()}")
+    current = _device()
+    if device.type != "cuda" or device.index != current:
+        raise ValueError(f"tensors on {device}, but the current device is cuda:{current}")
     for name, t in tensors.items():
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != current:
             raise ValueError(f"{name} is on {t.device}, expected {device}")
 
 
 def _int32(name: str, t: Optional[torch.Tensor], *shape: int) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: contiguous int32 {list(shape)} expected, got {t.dtype} {list(t.shape)}")
     return t.data_ptr()
 
 
 def _rows(name: str, t: torch.Tensor, heads: int, dim: int, dtype: torch.dtype) -> Tuple[int, int]:
     """Address and token stride of [tokens][heads][dim] whose tokens may lie apart."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.dtype != dtype:
+    if t.dtype is not dtype or t.dim() != 3 or t.shape[1:] != (heads, dim):
         raise ValueError(f"{name}: {dtype} [tokens][{heads}][{dim}] expected, got {t.dtype} {list(t.shape)}")
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (t.shape[0] > 1 and t.stride(0) < heads * dim):
-        raise ValueError(f"{name}: the heads of a token must lie side by side, strides are {t.stride()}")
-    stride = t.stride(0) if t.shape[0] > 1 else heads * dim
-    if t.data_ptr() % 16 or stride * t.element_size() % 16:
+    stride, address = heads * dim, t.data_ptr()
+    if not t.is_contiguous():
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (t.size(0) > 1 and t.stride(0) < stride):
+            raise ValueError(f"{name}: the heads of a token must lie side by side, strides are {t.stride()}")
+        if t.size(0) > 1:
+            stride = t.stride(0)
+    if address % 16 or stride * t.element_size() % 16:
         raise ValueError(f"{name}: tokens must start on 16-byte boundaries")
-    return t.data_ptr(), stride
+    return address, stride
 
 
 def _output(out: Optional[torch.Tensor], like: torch.Tensor) -> torch.Tensor:
     if out is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
     if out.dtype != like.dtype or out.shape != like.shape or not out.is_contiguous() or out.device != like.device:
         raise ValueError(f"out: contiguous {like.dtype} {list(like.shape)} on {like.device} expected")
     return out
 
 
 def _seqs(seq_start: torch.Tensor) -> int:
-    if seq_start.dim() != 1 or seq_start.shape[0] < 1:
+    n = seq_start.numel()
+    if seq_start.dim() != 1 or n < 1:
         raise ValueError("seq_start: [n_seq + 1] expected")
-    return seq_start.shape[0] - 1
+    return n - 1
 
 
 class KVCache:
@@ -634,10 +641,10 @@ def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, page_table: torc
         ws = None
         if need.value:
             if stream is None:
-                ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+                ws = q.new_empty(need.value, dtype=torch.uint8)
             else:
                 with torch.cuda.stream(stream):
-                    ws = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+                    ws = q.new_empty(need.value, dtype=torch.uint8)
         rc = lib.s2moe_tree_attention(cache._ref, int(layer), n_seq, n, heads, qp, qs, table, width, ctx, starts, n_nodes, nodes,
                                       par, dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
                                       None if ws is None else ws.data_ptr(), need.value, _stream_handle(stream))
@@ -698,11 +705,10 @@ def kv_copy_pages(cache: KVCache, pairs: Sequence[Tuple[int, int]], stream: Opti
     ``PagePool.reserve`` or ``PagePool.compact`` returned."""
     lib = load_library()
     _on_device(cache.device)
-    flat = [int(x) for pair in pairs for x in pair]
+    flat = array.array("i", itertools.chain.from_iterable(pairs))
     if len(flat) != 2 * len(pairs):
         raise ValueError("pairs: (from, to)")
-    arr = (ctypes.c_int32 * max(1, len(flat)))(*flat)
-    rc = lib.s2moe_kv_copy_pages(cache._ref, len(pairs), ctypes.cast(arr, ctypes.c_void_p), _stream_handle(stream))
+    rc = lib.s2moe_kv_copy_pages(cache._ref, len(pairs), flat.buffer_info()[0], _stream_handle(stream))
     if rc != OK:
         raise S2MoEError(rc, "s2moe_kv_copy_pages")
 

@@ -31,17 +31,27 @@ bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 int elem_size(int dtype) { return dtype == S2MOE_F32 ? 4 : 2; }
 bool head_dim_ok(int d) { return d == 64 || d == 128; }
 
-int *status_word()
+// What does not change while the process lives, per device: looked up once, then read without a call.
+struct DeviceFacts {
+    std::atomic<int> n_sm{0};
+    std::atomic<int *> status{nullptr};
+};
+constexpr int kDevices = 64;
+DeviceFacts *device_facts(int *dev_out = nullptr)
 {
+    static DeviceFacts facts[kDevices];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return nullptr;
+    if (dev_out) *dev_out = dev;
+    DeviceFacts *f = &facts[dev];
+    if (f->n_sm.load(std::memory_order_acquire) > 0) return f;
+    int n = 0;
     void *p = nullptr;
-    return cudaGetSymbolAddress(&p, g_attn_status) == cudaSuccess ? static_cast<int *>(p) : nullptr;
-}
-
-int sm_count()
-{
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || cudaGetSymbolAddress(&p, g_attn_status) != cudaSuccess)
+        return nullptr;
+    f->status.store(static_cast<int *>(p), std::memory_order_relaxed);
+    f->n_sm.store(n, std::memory_order_release);
+    return f;
 }
 
 // 0 or a negative status
@@ -75,6 +85,7 @@ int launch_status() { return cudaGetLastError() == cudaSuccess ? S2MOE_OK : S2MO
 struct TreePlan {
     int rows_tile, grid, min_units, key_tile;
     bool split, pair;
+    bool countable;                // the kernels count the units of a call in 32 bits
     int64_t items;                 // upper bound
     int64_t workspace;
 };
@@ -100,6 +111,8 @@ TreePlan tree_plan(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_hea
         p.grid = n_sm;
     }
     p.items = (int64_t)n_kv_heads * (rows / p.rows_tile + (n_tokens < n_seq ? n_tokens : n_seq));
+    const int64_t tiles = (capacity + p.key_tile - 1) / p.key_tile;
+    p.countable = n_kv_heads * (rows / p.rows_tile + 1) * tiles < kAttnMaxUnits && p.items * tiles <= INT32_MAX;
     p.split = capacity > (int64_t)p.min_units * p.key_tile;
     p.workspace = p.split ? (int64_t)p.grid * 2 * p.rows_tile * (head_dim + 2) * 4 : 0;
     return p;
@@ -135,11 +148,20 @@ bool make_map(CUtensorMap *m, const void *base, int64_t n0, int64_t n1, int64_t 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename K, typename... A>
-int launch(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, bool behind, A... args)
+// `Kernel` is a template argument so that each kernel has its own record of the devices on which its shared-memory limit
+// has been raised.  behind: may start before the kernel in front of it has ended (and waits for that itself).
+template <auto Kernel, typename... A>
+int launch(int64_t grid, int threads, size_t smem, cudaStream_t st, bool behind, const A &...args)
 {
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-        return S2MOE_ECUDA;
+    if (smem > 48 * 1024) {
+        static std::atomic<uint64_t> raised{0};
+        int dev = 0;
+        if (!device_facts(&dev)) return S2MOE_ECUDA;
+        if (!(raised.load(std::memory_order_relaxed) >> dev & 1)) {
+            if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return S2MOE_ECUDA;
+            raised.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
+    }
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
@@ -150,7 +172,7 @@ int launch(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, b
     lc.stream = st;
     lc.attrs = &attr;
     lc.numAttrs = behind ? 1 : 0;
-    return cudaLaunchKernelEx(&lc, kernel, args...) == cudaSuccess ? S2MOE_OK : S2MOE_ECUDA;
+    return cudaLaunchKernelEx(&lc, Kernel, args...) == cudaSuccess ? S2MOE_OK : S2MOE_ECUDA;
 }
 
 int64_t grid_for(int64_t items) { return items < (1 << 20) ? items : 1 << 20; }
@@ -158,13 +180,13 @@ int64_t grid_for(int64_t items) { return items < (1 << 20) ? items : 1 << 20; }
 template <int D, int R, bool PAGED, bool SPLIT>
 int launch_simple(const AttnArgs &a, int64_t grid, cudaStream_t st)
 {
-    return launch(attn_simple_kernel<float, D, R, PAGED, SPLIT>, grid, kAttnSimpleThreads, (size_t)attn_simple_smem(D, R), st, false, a);
+    return launch<attn_simple_kernel<float, D, R, PAGED, SPLIT>>(grid, kAttnSimpleThreads, (size_t)attn_simple_smem(D, R), st, false, a);
 }
 
 template <int D, bool PAGED, bool PAIR, bool SPLIT>
 int launch_tc(const AttnMaps &maps, const AttnArgs &a, int64_t grid, cudaStream_t st)
 {
-    return launch(attn_tc_kernel<D, PAGED, PAIR, SPLIT>, grid, kAttnThreads, (size_t)AttnSmem<D, PAIR>::bytes, st, false, maps, a);
+    return launch<attn_tc_kernel<D, PAGED, PAIR, SPLIT>>(grid, kAttnThreads, (size_t)AttnSmem<D, PAIR>::bytes, st, false, maps, a);
 }
 
 template <int D>
@@ -189,13 +211,13 @@ int run_tree(int dtype, AttnArgs a, const TreePlan &p, cudaStream_t st)
 {
     a.rows_tile = p.rows_tile;
     a.min_units = p.min_units;
-    const int64_t grid = p.split ? p.grid : grid_for(p.items), join = ((int64_t)a.n_tokens * a.Hk + 3) / 4;
+    const int64_t grid = p.split ? p.grid : grid_for(p.items), join = ((int64_t)a.n_tokens * a.Hk * a.group + 3) / 4;
     int rc;
     if (dtype == S2MOE_F32) {
         if (p.rows_tile == 16) rc = p.split ? launch_simple<D, 16, true, true>(a, grid, st) : launch_simple<D, 16, true, false>(a, grid, st);
         else rc = p.split ? launch_simple<D, 64, true, true>(a, grid, st) : launch_simple<D, 64, true, false>(a, grid, st);
         if (rc != S2MOE_OK || !p.split) return rc;
-        return launch(attn_join_kernel<float, D, kAttnSimpleTile>, join, 128, 0, st, true, a, p.grid);
+        return launch<attn_join_kernel<float, D, kAttnSimpleTile>>(join, 128, 0, st, true, a, p.grid);
     }
     const int page = 1 << a.page_shift;
     const int64_t rows = (int64_t)a.n_pages * a.Hk;
@@ -207,7 +229,7 @@ int run_tree(int dtype, AttnArgs a, const TreePlan &p, cudaStream_t st)
     if (p.pair) rc = p.split ? launch_tc<D, true, true, true>(maps, a, grid, st) : launch_tc<D, true, true, false>(maps, a, grid, st);
     else rc = p.split ? launch_tc<D, true, false, true>(maps, a, grid, st) : launch_tc<D, true, false, false>(maps, a, grid, st);
     if (rc != S2MOE_OK || !p.split) return rc;
-    return launch(attn_join_kernel<__nv_bfloat16, D, kAttnTile>, join, 128, 0, st, true, a, p.grid);
+    return launch<attn_join_kernel<__nv_bfloat16, D, kAttnTile>>(join, 128, 0, st, true, a, p.grid);
 }
 
 }  // namespace
@@ -228,7 +250,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     if (q_stride % per16 || k_stride % per16 || v_stride % per16) return S2MOE_EINVAL;
     if (q_stride < (int64_t)n_heads * head_dim || k_stride < (int64_t)n_kv_heads * head_dim || v_stride < (int64_t)n_kv_heads * head_dim)
         return S2MOE_EINVAL;
-    if ((int64_t)n_tokens * n_heads > kMaxRows) return S2MOE_ERANGE;
+    if ((int64_t)n_tokens * n_heads > kMaxRows || (int64_t)n_seq * n_kv_heads > kMaxRows) return S2MOE_ERANGE;
     AttnArgs a{};
     a.q = q; a.k = k; a.v = v; a.out = out;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
@@ -236,8 +258,9 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     a.n_seq = n_seq; a.n_tokens = a.n_nodes = n_tokens; a.Hk = n_kv_heads; a.group = n_heads / n_kv_heads;
     a.min_units = 1;
     a.scale_log2 = scale * 1.44269504f;
-    a.status = status_word();
-    if (!a.status) return S2MOE_ECUDA;
+    const DeviceFacts *facts = device_facts();
+    if (!facts) return S2MOE_ECUDA;
+    a.status = facts->status;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     return head_dim == 64 ? run_prompt<64>(dtype, a, st) : run_prompt<128>(dtype, a, st);
 }
@@ -251,8 +274,9 @@ int s2moe_tree_attention_workspace(const s2moe_kv_cache *cache, int32_t n_seq, i
     if (rc != S2MOE_OK) return rc;
     if (n_seq < 0 || n_tokens < 0 || table_width < 1 || !heads_ok(n_heads, cache->n_kv_heads)) return S2MOE_EINVAL;
     if (n_seq == 0 || n_tokens == 0) return S2MOE_OK;
-    const int n_sm = sm_count();
-    if (n_sm < 1) return S2MOE_ECUDA;
+    const DeviceFacts *facts = device_facts();
+    if (!facts) return S2MOE_ECUDA;
+    const int n_sm = facts->n_sm;
     *bytes = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads, (int64_t)table_width * cache->page_size,
                        cache->head_dim, n_sm).workspace;
     return S2MOE_OK;
@@ -274,10 +298,12 @@ int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_s
     if (!aligned16(q) || !aligned16(out) || q_stride % (16 / elem_size(cache->dtype)) || q_stride < (int64_t)n_heads * cache->head_dim)
         return S2MOE_EINVAL;
     if ((int64_t)n_tokens * n_heads > kMaxRows || (int64_t)table_width * cache->page_size > INT32_MAX - 128) return S2MOE_ERANGE;
-    const int n_sm = sm_count();
-    if (n_sm < 1) return S2MOE_ECUDA;
+    const DeviceFacts *facts = device_facts();
+    if (!facts) return S2MOE_ECUDA;
+    const int n_sm = facts->n_sm;
     const TreePlan p = tree_plan(cache->dtype, n_seq, n_tokens, n_heads, cache->n_kv_heads,
                                  (int64_t)table_width * cache->page_size, cache->head_dim, n_sm);
+    if (!p.countable) return S2MOE_ERANGE;
     if (p.workspace > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < p.workspace)) return S2MOE_EINVAL;
     const int64_t layer_bytes = (int64_t)cache->n_pages * cache->n_kv_heads * cache->page_size * cache->head_dim * elem_size(cache->dtype);
     AttnArgs a{};
@@ -293,8 +319,7 @@ int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_s
     a.scale_log2 = scale * 1.44269504f;
     a.part_o = (float *)workspace;
     a.part_ml = (float *)workspace + (int64_t)p.grid * 2 * p.rows_tile * cache->head_dim;
-    a.status = status_word();
-    if (!a.status) return S2MOE_ECUDA;
+    a.status = facts->status;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     return cache->head_dim == 64 ? run_tree<64>(cache->dtype, a, p, st) : run_tree<128>(cache->dtype, a, p, st);
 }

@@ -19,6 +19,7 @@
 
 namespace s2moe {
 
+constexpr int kAttnMaxUnits = 1 << 26;     // units of one sequence
 constexpr int kAttnMaxNodes = 64;         // nodes of a tree with parents: one bit each
 
 struct AttnArgs {
@@ -84,6 +85,36 @@ __device__ __forceinline__ unsigned long long attn_ancestors(const AttnArgs &a, 
     return m;
 }
 
+// The same for every node of a tree of up to 64, by a whole warp: lane l gets nodes l and l + 32.  Pointers are doubled,
+// so a chain of 64 takes 6 rounds of shuffles, not 64 loads one behind the other.
+__device__ __forceinline__ void attn_ancestors_all(const AttnArgs &a, const AttnSeq &q, unsigned long long (&m)[2])
+{
+    const int lane = threadIdx.x & 31;
+    int up[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int i = lane + 32 * j, p = i < q.nodes ? __ldg(a.parent + q.node0 + i) : -1;
+        up[j] = p < i && p >= 0 ? p : -1;
+        m[j] = 1ull << i;
+    }
+    while (__any_sync(0xffffffffu, up[0] >= 0 || up[1] >= 0)) {
+        unsigned long long add[2];
+        int nx[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const unsigned long long lo = __shfl_sync(0xffffffffu, m[0], up[j] & 31), hi = __shfl_sync(0xffffffffu, m[1], up[j] & 31);
+            const int ul = __shfl_sync(0xffffffffu, up[0], up[j] & 31), uh = __shfl_sync(0xffffffffu, up[1], up[j] & 31);
+            add[j] = up[j] < 0 ? 0ull : up[j] < 32 ? lo : hi;
+            nx[j] = up[j] < 0 ? -1 : up[j] < 32 ? ul : uh;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            m[j] |= add[j];
+            up[j] = nx[j];
+        }
+    }
+}
+
 // first key behind those that token t of the sequence sees, ancestry aside
 template <bool PAGED>
 __device__ __forceinline__ int attn_limit(const AttnSeq &q, int t)
@@ -115,15 +146,6 @@ __device__ __forceinline__ bool attn_key(const AttnArgs &a, const AttnSeq &q, in
 
 // ---- the split ---------------------------------------------------------------------------------------------------
 
-template <int KEY_TILE>
-struct AttnCut {
-    __device__ static int tiles(const AttnSeq &q) { return max(1, (q.total + KEY_TILE - 1) / KEY_TILE); }
-    __device__ static int row_tiles(const AttnArgs &a, const AttnSeq &q)
-    {
-        return (int)(((long long)q.n * a.group + a.rows_tile - 1) / a.rows_tile);
-    }
-};
-
 struct AttnPiece {
     int s, h, rt;                // sequence, key/value head, block of rows
     int t0, t1;                  // key tiles
@@ -131,107 +153,145 @@ struct AttnPiece {
     AttnSeq q;
 };
 
-// Walks the pieces of one CTA; every warp that needs them walks for itself, all 32 lanes together.
-// SPLIT: units are key tiles and a CTA takes one range of them; otherwise units are items and a CTA takes every
-// gridDim.x-th (prompts: the blocks of a sequence with the most keys first, its heads side by side).
+// `w` units cut into ranges whose sizes differ by one at most
+struct AttnCut {
+    int ctas, each, more;        // CTAs that take part, units of each, the first `more` take one more
+    __device__ AttnCut(const AttnArgs &a, int w, int grid)
+    {
+        ctas = max(1, min(grid, w / a.min_units));
+        each = w / ctas;
+        more = w - each * ctas;
+    }
+    __device__ int start(int c) const { return c * each + min(c, more); }
+    __device__ int owner(int u) const
+    {
+        const int wide = more * (each + 1);
+        return u < wide ? u / (each + 1) : more + (u - wide) / each;
+    }
+};
+
+// Finds the pieces of one CTA; every warp that needs them looks for itself, all 32 lanes together.  32 sequences at a
+// time are held by the lanes, so that one round of loads serves all that follows (the host refuses calls with more
+// than 2^31 units).
+// SPLIT: units are key tiles, in the order sequence, head, block, tile, and next() walks the CTA's range of them.
+// Otherwise units are items and item(u, p) gives one: blocks with the most keys in front of them come first, across the
+// sequences held, so that CTAs that take items as they become free end together.
 template <bool PAGED, bool SPLIT, int KEY_TILE>
 struct AttnIter {
-    using Cut = AttnCut<KEY_TILE>;
     const AttnArgs &a;
     const int lane;
-    int s = -1;
-    long long base = 0, units = 0;       // first unit and units of sequence s
-    long long u = 0, u_end = 0;
-    AttnSeq q{};
+    int chunk = 0, base = 0, units = 0;          // first sequence held, units before them, their units
+    AttnSeq mine;                                // this lane's sequence
+    int my = 0, inc = 0, rts = 0;                // its units, the same summed up to this lane, its blocks of rows
+    int level = 0, level_base = 0;
+    int u = 0, u_end = 0;
     bool first = true;
 
     __device__ AttnIter(const AttnArgs &args, int lane_) : a(args), lane(lane_) {}
 
-    __device__ long long units_of(int i) const
+    __device__ static int tiles(const AttnSeq &q) { return max(1, (q.total + KEY_TILE - 1) / KEY_TILE); }
+    __device__ int row_tiles(const AttnSeq &q) const { return (q.n * a.group + a.rows_tile - 1) / a.rows_tile; }
+    __device__ void load(int c)
     {
-        const AttnSeq x = attn_seq<PAGED>(a, i);
-        return (long long)a.Hk * Cut::row_tiles(a, x) * (SPLIT ? Cut::tiles(x) : 1);
-    }
-    __device__ bool seek(long long unit)
-    {
-        if (unit < base + units) return true;
-        long long b = base + units;
-        for (int s0 = s + 1; s0 < a.n_seq; s0 += 32) {
-            const int mine = s0 + lane;
-            const long long un = mine < a.n_seq ? units_of(mine) : 0;
-            long long inc = un;
+        chunk = c;
+        mine = AttnSeq{};
+        if (c + lane < a.n_seq) mine = attn_seq<PAGED>(a, c + lane);
+        rts = row_tiles(mine);
+        const long long want = (long long)a.Hk * rts * (SPLIT ? tiles(mine) : 1);
+        if (want >= kAttnMaxUnits) rts = 0;
+        my = inc = want >= kAttnMaxUnits ? 0 : (int)want;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long t = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += t;
-            }
-            const unsigned hit = __ballot_sync(0xffffffffu, b + inc > unit);
-            if (hit) {
-                const int l = __ffs((int)hit) - 1;
-                s = s0 + l;
-                base = b + __shfl_sync(0xffffffffu, inc - un, l);
-                units = __shfl_sync(0xffffffffu, un, l);
-                q = attn_seq<PAGED>(a, s);
-                return true;
-            }
-            b += __shfl_sync(0xffffffffu, inc, 31);
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += t;
         }
-        return false;
+        units = __shfl_sync(0xffffffffu, inc, 31);
+        if (!SPLIT) {
+            level = __reduce_max_sync(0xffffffffu, rts) - 1;
+            level_base = 0;
+        }
     }
-    __device__ long long total_units() const
+    // units of all sequences, once the first 32 are held
+    __device__ int all_units() const
     {
+        if (a.n_seq <= 32) return units;
         long long w = 0;
-        for (int i = lane; i < a.n_seq; i += 32) w += units_of(i);
+        for (int i = 32 + lane; i < a.n_seq; i += 32) {
+            const AttnSeq x = attn_seq<PAGED>(a, i);
+            const long long want = (long long)a.Hk * row_tiles(x) * tiles(x);
+            if (want < kAttnMaxUnits) w += want;
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-        return w;
+        return (int)min(w + units, (long long)INT32_MAX);
     }
-    // CTAs that take part in a split of w units
-    __device__ static long long ctas(const AttnArgs &a, long long w, int grid)
+    __device__ bool hold(int unit)
     {
-        return max(1ll, min((long long)grid, w / a.min_units));
+        while (unit - base >= units) {
+            if (chunk + 32 >= a.n_seq || units > INT32_MAX - base) return false;
+            base += units;
+            load(chunk + 32);
+        }
+        return true;
+    }
+    __device__ void take(int l, AttnPiece &p) const
+    {
+        p.s = chunk + l;
+        p.q.tok0 = __shfl_sync(0xffffffffu, mine.tok0, l);
+        p.q.n = __shfl_sync(0xffffffffu, mine.n, l);
+        p.q.node0 = PAGED ? __shfl_sync(0xffffffffu, mine.node0, l) : p.q.tok0;
+        p.q.nodes = PAGED ? __shfl_sync(0xffffffffu, mine.nodes, l) : p.q.n;
+        p.q.ctx = PAGED ? __shfl_sync(0xffffffffu, mine.ctx, l) : 0;
+        p.q.total = PAGED ? __shfl_sync(0xffffffffu, mine.total, l) : p.q.n;
+        p.q.bad = PAGED ? __shfl_sync(0xffffffffu, (int)mine.bad, l) != 0 : false;
     }
     __device__ void begin()
     {
+        load(0);
         if (SPLIT) {
-            const long long w = total_units(), g = ctas(a, w, (int)gridDim.x);
-            if (blockIdx.x < g) {
-                u = w * blockIdx.x / g;
-                u_end = w * (blockIdx.x + 1) / g;
+            const AttnCut cut(a, all_units(), (int)gridDim.x);
+            if ((int)blockIdx.x < cut.ctas) {
+                u = cut.start((int)blockIdx.x);
+                u_end = cut.start((int)blockIdx.x + 1);
             }
-        } else {
-            u = blockIdx.x;
-            u_end = 1ll << 62;
         }
     }
     __device__ bool next(AttnPiece &p)
     {
-        if (u >= u_end || !seek(u)) return false;
-        p.s = s;
-        p.q = q;
-        const int rts = Cut::row_tiles(a, q);
-        if (SPLIT) {
-            const int tiles = Cut::tiles(q);
-            const int rel = (int)(u - base), item = rel / tiles;
-            p.h = item / rts;
-            p.rt = item - p.h * rts;
-            p.t0 = rel - item * tiles;
-            p.t1 = (int)min((long long)tiles, p.t0 + (u_end - u));
-            // an unfinished item is the CTA's first (place 0) or its last (place 1)
-            p.slot = p.t0 == 0 && p.t1 == tiles ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
-            first = false;
-            u += p.t1 - p.t0;
-        } else {
-            const int rel = (int)(u - base), r = rel / a.Hk;
-            p.h = rel - r * a.Hk;
-            p.rt = PAGED ? r : rts - 1 - r;
-            p.t0 = 0;
-            // no key behind the last row's own is needed
-            const int last = min(q.n, ((p.rt + 1) * a.rows_tile + a.group - 1) / a.group) - 1;
-            p.t1 = max(1, (attn_limit<PAGED>(q, last) + KEY_TILE - 1) / KEY_TILE);
-            p.slot = -1;
-            u += gridDim.x;
+        if (u >= u_end || !hold(u)) return false;
+        const int l = __ffs((int)__ballot_sync(0xffffffffu, inc > u - base)) - 1;
+        take(l, p);
+        const int rel = u - base - __shfl_sync(0xffffffffu, inc - my, l), n = tiles(p.q), item = rel / n;
+        const int blocks = __shfl_sync(0xffffffffu, rts, l);
+        p.h = item / blocks;
+        p.rt = item - p.h * blocks;
+        p.t0 = rel - item * n;
+        p.t1 = min(n, p.t0 + (u_end - u));
+        // an unfinished item is the CTA's first (place 0) or its last (place 1)
+        p.slot = p.t0 == 0 && p.t1 == n ? -1 : 2 * (int)blockIdx.x + (first ? 0 : 1);
+        first = false;
+        u += p.t1 - p.t0;
+        return true;
+    }
+    __device__ bool item(int unit, AttnPiece &p)
+    {
+        if (!hold(unit)) return false;
+        unsigned have = __ballot_sync(0xffffffffu, rts > level);
+        while (unit - base >= level_base + __popc(have) * a.Hk) {
+            level_base += __popc(have) * a.Hk;
+            --level;
+            have = __ballot_sync(0xffffffffu, rts > level);
         }
+        const int rel = unit - base - level_base, k = rel / a.Hk;
+        const unsigned hit = __ballot_sync(0xffffffffu, ((have >> lane) & 1u) && __popc(have & ((1u << lane) - 1u)) == k);
+        take(__ffs((int)hit) - 1, p);
+        p.h = rel - k * a.Hk;
+        p.rt = level;
+        p.t0 = 0;
+        // no key behind the last row's own is needed
+        const int last = min(p.q.n, ((level + 1) * a.rows_tile + a.group - 1) / a.group) - 1;
+        p.t1 = max(1, (attn_limit<PAGED>(p.q, last) + KEY_TILE - 1) / KEY_TILE);
+        p.slot = -1;
         return true;
     }
 };

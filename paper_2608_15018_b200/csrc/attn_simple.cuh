@@ -71,7 +71,9 @@ __global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(Attn
     AttnIter<PAGED, SPLIT, kAttnSimpleTile> it(a, lane);
     AttnPiece p;
     it.begin();
-    while (it.next(p)) {
+    int unit = blockIdx.x;
+    while (SPLIT ? it.next(p) : it.item(unit, p)) {
+        unit += gridDim.x;
         const AttnSeq &q = p.q;
         const int rows = q.n * a.group, row0 = p.rt * R;
         __syncthreads();
@@ -228,78 +230,79 @@ __global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(Attn
     }
 }
 
-// Joins the pieces of the items that the split cut: one warp per token and key/value head.
+// Joins the pieces of the items that the split cut: one warp per token and query head, D / 32 columns per lane.
 //   M = max m_i, out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M)
+// The kernel in front may still run: what depends on the lengths alone is worked out before the wait for its end.
 template <typename T, int D, int KEY_TILE>
 __global__ void __launch_bounds__(128) attn_join_kernel(AttnArgs a, int grid)
 {
-    using Cut = AttnCut<KEY_TILE>;
     constexpr int C = D / 32;
-    const int lane = threadIdx.x & 31;
-    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int tok = (int)(unit / a.Hk), h = (int)(unit - (long long)tok * a.Hk);
+    const int lane = threadIdx.x & 31, Hq = a.Hk * a.group;
+    const long long row_id = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int tok = (int)(row_id / Hq), head = (int)(row_id - (long long)tok * Hq), h = head / a.group;
     AttnIter<true, true, KEY_TILE> it(a, lane);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (tok >= a.n_tokens) return;
-    const long long w = it.total_units(), g = it.ctas(a, w, grid);
-    // the sequence of this token, and the units in front of it
-    long long base = 0;
-    int s = -1;
-    for (int s0 = 0; s0 < a.n_seq && s < 0; s0 += 32) {
-        long long un = 0;
-        bool mine = false;
-        if (s0 + lane < a.n_seq) {
-            const AttnSeq x = attn_seq<true>(a, s0 + lane);
-            mine = tok >= x.tok0 && tok < x.tok0 + x.n;
-            un = it.units_of(s0 + lane);
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, mine);
-        if (hit) s = s0 + __ffs((int)hit) - 1;
-        if (hit && lane >= __ffs((int)hit) - 1) un = 0;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) un += __shfl_xor_sync(0xffffffffu, un, o);
-        base += un;
+    it.load(0);
+    const AttnCut cut(a, it.all_units(), grid);
+    // the sequence of this token
+    unsigned hit = 0;
+    while (tok < a.n_tokens) {
+        hit = __ballot_sync(0xffffffffu, tok >= it.mine.tok0 && tok < it.mine.tok0 + it.mine.n);
+        if (hit || it.chunk + 32 >= a.n_seq) break;
+        it.base += it.units;
+        it.load(it.chunk + 32);
     }
-    if (s < 0) return;
-    const AttnSeq q = attn_seq<true>(a, s);
-    const int tiles = Cut::tiles(q), rts = Cut::row_tiles(a, q), t = tok - q.tok0;
-    for (int gr = 0; gr < a.group; ++gr) {
-        const int row = t * a.group + gr, rt = row / a.rows_tile, r = row - rt * a.rows_tile;
-        const long long u0 = base + ((long long)h * rts + rt) * tiles, u1 = u0 + tiles;
-        const long long c0 = ((u0 + 1) * g - 1) / w, c1 = (u1 * g - 1) / w;       // CTAs of the first and the last unit
-        if (c0 == c1) continue;                                                // a whole item: written already
-        float m = -CUDART_INF_F, l = 0.f, o[C];
+    AttnPiece p;
+    int c0 = 0, c1 = 0, t = 0, r = 0, u0 = 0;
+    if (hit) {
+        const int l = __ffs((int)hit) - 1;
+        it.take(l, p);
+        t = tok - p.q.tok0;
+        const int tiles = it.tiles(p.q), row = t * a.group + head - h * a.group, rt = row / a.rows_tile;
+        r = row - rt * a.rows_tile;
+        u0 = it.base + __shfl_sync(0xffffffffu, it.inc - it.my, l) + (h * __shfl_sync(0xffffffffu, it.rts, l) + rt) * tiles;
+        c0 = cut.owner(u0);
+        c1 = cut.owner(u0 + tiles - 1);
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!hit || c0 == c1) return;                              // a whole item: written already
+    float m = -CUDART_INF_F, l = 0.f, o[C];
 #pragma unroll
-        for (int i = 0; i < C; ++i) o[i] = 0.f;
-        for (long long c = c0; c <= c1; ++c) {
-            const long long slot = 2 * c + (c == c0 && w * c / g < u0 ? 1 : 0);
-            const long long at = slot * a.rows_tile + r;
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
-            const float mn = fmaxf(m, ml.x), b = mn == -CUDART_INF_F ? 0.f : mn;
-            const float f = exp2f(m - b), e = exp2f(ml.x - b);
-            m = mn;
-            l = l * f + ml.y * e;
+    for (int i = 0; i < C; ++i) o[i] = 0.f;
+#pragma unroll 2
+    for (int c = c0; c <= c1; ++c) {
+        const long long at = (2ll * c + (c == c0 && cut.start(c) < u0 ? 1 : 0)) * a.rows_tile + r;
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
+        float x[C];
+        if (C == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * lane);
+        else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(a.part_o + at * D + 2 * lane);
+        const float mn = fmaxf(m, ml.x), b = mn == -CUDART_INF_F ? 0.f : mn;
+        const float f = exp2f(m - b), e = exp2f(ml.x - b);
+        m = mn;
+        l = l * f + ml.y * e;
 #pragma unroll
-            for (int i = 0; i < C; ++i) o[i] = o[i] * f + a.part_o[at * D + lane + 32 * i] * e;
+        for (int i = 0; i < C; ++i) o[i] = o[i] * f + x[i] * e;
+    }
+    const float inv = p.q.bad ? CUDART_NAN_F : 1.f / l;
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        o[i] *= inv;
+        fine = fine && attn_finite(o[i]);
+    }
+    T *dst = reinterpret_cast<T *>(a.out) + ((long long)tok * Hq + head) * D;
+    if (!p.q.bad && __any_sync(0xffffffffu, !fine)) {
+        float x[C];
+        if (attn_row_again<T, D, true>(a, p.q, p.s, h, t, head, p.q.total, l == 0.f, x)) {
+#pragma unroll
+            for (int i = 0; i < C; ++i) dst[lane + 32 * i] = (T)x[i];
+            return;
         }
-        const int head = h * a.group + gr;
-        const float inv = q.bad ? CUDART_NAN_F : 1.f / l;
-        bool fine = true;
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            o[i] *= inv;
-            fine = fine && attn_finite(o[i]);
-        }
-        if (!q.bad && __any_sync(0xffffffffu, !fine)) {
-            float x[C];
-            if (attn_row_again<T, D, true>(a, q, s, h, t, head, q.total, l == 0.f, x)) {
-#pragma unroll
-                for (int i = 0; i < C; ++i) o[i] = x[i];
-            }
-        }
-        T *dst = reinterpret_cast<T *>(a.out) + ((long long)tok * a.Hk * a.group + head) * D;
-#pragma unroll
-        for (int i = 0; i < C; ++i) dst[lane + 32 * i] = (T)o[i];
+    }
+    if (C == 4) {
+        attn_store4(dst + 4 * lane, make_float4(o[0], o[1], o[C - 2], o[C - 1]));
+    } else {
+        dst[2 * lane] = (T)o[0];
+        dst[2 * lane + 1] = (T)o[1];
     }
 }
 

@@ -29,6 +29,7 @@ namespace s2moe {
 constexpr int kAttnTile = 128;
 constexpr int kAttnThreads = 384;                 // 8 softmax warps, matrix instructions, copies, two warps without work
 constexpr int kAttnHalf = 128 * 128;              // bytes of 128 rows x 64 columns
+constexpr int kAttnPoly = 2;                      // of 8 pairs of weights, those that take the polynomial
 constexpr float kAttnSlack = 8.f;                 // log2 of the largest weight before the maximum is moved
 
 template <int D, bool PAIR>
@@ -65,6 +66,46 @@ __device__ __forceinline__ void attn_ld_wait(float (&v)[N])
 }
 __device__ __forceinline__ void attn_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// two binary32 operations per instruction
+__device__ __forceinline__ float2 attn_fma2(float2 x, float2 y, float2 z)
+{
+    float2 r;
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t &>(r))
+        : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)), "l"(reinterpret_cast<uint64_t &>(z)));
+    return r;
+}
+__device__ __forceinline__ float2 attn_add2(float2 x, float2 y)
+{
+    float2 r;
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
+    return r;
+}
+__device__ __forceinline__ float2 attn_mul2(float2 x, float2 y)
+{
+    float2 r;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
+    return r;
+}
+
+// 2^x for two x <= 64 on the multiply-add pipe: x = n + r with n the nearest integer, 2^r for |r| <= 1/2 by a polynomial of
+// degree 4 (fitted for the smallest largest relative error, 2.7e-6 with its coefficients in binary32), 2^n put together as
+// a number.  x below -126 counts as -126, NaN stays NaN.
+__device__ __forceinline__ float2 attn_exp2_poly(float2 x)
+{
+    constexpr float kMagic = 12582912.f + 127.f;                  // 1.5 * 2^23: the sum's low bits are n + 127
+    asm("max.NaN.ftz.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+    asm("max.NaN.ftz.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+    const float2 t = attn_add2(x, make_float2(kMagic, kMagic));
+    const float2 n = attn_add2(t, make_float2(-kMagic, -kMagic));
+    const float2 r = attn_fma2(n, make_float2(-1.f, -1.f), x);
+    float2 y = attn_fma2(r, make_float2(0.009570102f, 0.009570102f), make_float2(0.055917859f, 0.055917859f));
+    y = attn_fma2(y, r, make_float2(0.24024744f, 0.24024744f));
+    y = attn_fma2(y, r, make_float2(0.69312179f, 0.69312179f));
+    y = attn_fma2(y, r, make_float2(0.99999928f, 0.99999928f));
+    return attn_mul2(y, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
+}
+
 // bits [0, n) of a word whose bits stand for keys from 32 * j on
 __device__ __forceinline__ uint32_t attn_prefix(int n, int j)
 {
@@ -79,7 +120,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     using Iter = AttnIter<PAGED, SPLIT, kAttnTile>;
     constexpr int NS = L::slots;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], p_full[2], ended;
+    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], p_half[2], p_full[2], ended, n_full[2], n_empty[2];
+    __shared__ __align__(16) uint4 next_cta[2];
     __shared__ uint32_t tmem_at;
     __shared__ float2 ml[2][128];
     uint8_t *qs = attn_raw + ((1024u - (smem_u32(attn_raw) & 1023u)) & 1023u), *ring = qs + L::q;
@@ -96,7 +138,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         mbar_init(&ended, 1);
         for (int w = 0; w < 2; ++w) {
             mbar_init(&s_full[w], 1);
+            mbar_init(&p_half[w], 4);
             mbar_init(&p_full[w], 4);
+            mbar_init(&n_full[w], 1);
+            mbar_init(&n_empty[w], 10);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -130,16 +175,55 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     Iter it(a, lane);
     AttnPiece p;
     unsigned r0 = 0;                                              // tiles of the pieces before
+    unsigned pieces = 0;
+    // Without a split the grid has a block per item, and a CTA that has an item under way takes the next block that has
+    // not started yet over (the hardware's work queue: no counter in memory, and no CTA waits for its start-up again).
+    // The copying warp asks one item ahead; all ten working warps read the answer.
+    auto next = [&]() -> bool {
+        if (SPLIT) return it.next(p);
+        int unit = (int)blockIdx.x;
+        if (pieces > 0) {
+            const unsigned k = pieces - 1, b = k & 1u;
+            wait(&n_full[b], (k >> 1) & 1u);
+            uint32_t got, x;
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+                "ld.shared.b128 r, [%2];\n\t"
+                "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t"
+                "mov.u32 %1, 0;\n\t"
+                "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+                : "=r"(got), "=r"(x)
+                : "r"(smem_u32(&next_cta[b]))
+                : "memory");
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&n_empty[b]);
+            if (!got || !__all_sync(0xffffffffu, ok)) return false;
+            unit = (int)x;
+        }
+        return it.item(unit, p);
+    };
 
     if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     it.begin();
     if (warp == 9) {
         // ------------------------------------------------------------------ copies
-        unsigned pieces = 0;
         const int ppt = PAGED ? kAttnTile >> a.page_shift : 1;
-        while (it.next(p) && __all_sync(0xffffffffu, ok)) {
+        while (next() && __all_sync(0xffffffffu, ok)) {
             const int nw = PAIR && p.rt * a.rows_tile + half < p.q.n * a.group ? 2 : 1;
+            if (!SPLIT) {                                         // the item after this one
+                const unsigned b = pieces & 1u;
+                wait(&n_empty[b], ((pieces >> 1) & 1u) ^ 1u);
+                if (lane == 0 && ok) {
+                    mbar_expect_tx(&n_full[b], 16);
+                    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                                     smem_u32(&next_cta[b])),
+                                 "r"(smem_u32(&n_full[b]))
+                                 : "memory");
+                }
+            }
             wait(&q_empty, (pieces & 1u) ^ 1u);
             if (lane == 0) {
                 mbar_expect_tx(&q_full, (uint32_t)(nw * (D / 64) * half * 128));
@@ -191,9 +275,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         // V: 64-column blocks kAttnHalf apart, groups of 8 keys 1024 bytes apart
         const uint64_t vd = (kd & ~(0x3fffull << 16)) | ((uint64_t)(kAttnHalf >> 4) << 16);
         const uint32_t k_hi = (uint32_t)(kd >> 32), v_hi = (uint32_t)(vd >> 32), q_hi = (uint32_t)(qd >> 32);
-        unsigned pieces = 0;
         uint32_t p_phase[2] = {0, 0};
-        while (it.next(p)) {
+        while (next()) {
             if (leader && ok) {
                 const int n[2] = {tiles_of(p, 0), tiles_of(p, 1)}, nt = p.t1 - p.t0;
                 auto scores = [&](int w, int t) {                 // S of group w from tile t of the piece
@@ -210,13 +293,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 auto product = [&](int w, int t, bool first) {    // O of group w from its weights and tile t
                     const unsigned c = 2 * (r0 + t) + 1, slot = c % NS;
                     wait(&full[slot], (c / NS) & 1u);
-                    wait(&p_full[w], p_phase[w]);
-                    p_phase[w] ^= 1u;
+                    wait(&p_half[w], p_phase[w]);
                     tc_fence_after();
                     const uint32_t vl = (uint32_t)vd + slot * (L::tile >> 4);
 #pragma unroll
-                    for (int k = 0; k < kAttnTile / 16; ++k)
+                    for (int k = 0; k < kAttnTile / 16; ++k) {
+                        if (k == kAttnTile / 32) {
+                            wait(&p_full[w], p_phase[w]);
+                            tc_fence_after();
+                        }
                         tc_mma_bf16_tmem_a(tmem_o[w], tmem_s[w] + 8 * k, vl + k * 128, v_hi, idesc_o, !first || k > 0);
+                    }
+                    p_phase[w] ^= 1u;
                 };
                 auto release = [&](int t, int kv) { tc_commit(&empty[(2 * (r0 + t) + kv) % NS]); };
                 wait(&q_full, pieces & 1u);
@@ -281,15 +369,15 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         const uint32_t s_at = tmem_s[w] + lanes, o_at = tmem_o[w] + lanes;
         const int ppt = PAGED ? kAttnTile >> a.page_shift : 0;
         uint32_t s_phase = 0;
-        while (it.next(p)) {
+        while (next()) {
             const AttnSeq &q = p.q;
             const int n = tiles_of(p, w), row = p.rt * a.rows_tile + (PAIR ? w * half : 0) + row_in;
             const bool mine = row_in < half && row < q.n * a.group, used = __any_sync(0xffffffffu, mine);
             const int token = mine ? row / a.group : 0, head = p.h * a.group + (mine ? row % a.group : 0);
             const int lim = mine ? attn_limit<PAGED>(q, token) : q.total;
             const bool tree = PAGED && a.parent && !q.bad;
-            unsigned long long anc = ~0ull;
-            if (tree && mine && p.t1 * kAttnTile > q.ctx) anc = attn_ancestors(a, q, q.nodes - q.n + token);
+            unsigned long long anc = 0;
+            bool have_anc = !tree;
             // keys below this one every row of the warp sees
             int clear = tree ? min(lim, q.ctx) : lim;
 #pragma unroll
@@ -305,6 +393,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         have = (unsigned)__ldg(a.page_table + (long long)p.s * a.table_width + at) < (unsigned)a.n_pages;
                     there = __ballot_sync(0xffffffffu, have);
                     all = (1u << ppt) - 1u;
+                }
+                if (!have_anc && key0 + kAttnTile > q.ctx) {        // the first tile with nodes of the tree
+                    have_anc = true;
+                    unsigned long long all_nodes[2];
+                    attn_ancestors_all(a, q, all_nodes);
+                    const int node = min(max(q.nodes - q.n + token, 0), kAttnMaxNodes - 1);
+                    const unsigned long long lo = __shfl_sync(0xffffffffu, all_nodes[0], node & 31), hi = __shfl_sync(0xffffffffu, all_nodes[1], node & 31);
+                    anc = node < 32 ? lo : hi;
                 }
                 wait(&s_full[w], s_phase);
                 s_phase ^= 1u;
@@ -325,79 +421,133 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 if (!used) {                                      // no row of the warp is in use: its lanes hold what they hold
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[w]);
+                    if (lane == 0) {
+                        mbar_arrive(&p_half[w]);
+                        mbar_arrive(&p_full[w]);
+                    }
                     continue;
                 }
-                float s[kAttnTile];
+                // the maximum in use becomes `top` where that is larger by more than the slack (at first: always)
+                auto settle = [&](float top) -> float {
+                    const bool move = top > m + kAttnSlack;        // m = -inf: any
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float f = move ? exp2f(m - top) : 1.f;
+                        if (move) m = top;
+                        l *= f;
+                        if (i > 0) {                              // the product before this tile has ended: S came behind it
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                float o[32];
+                                attn_ld32(o_at + 32 * c, o);
+                                attn_ld_wait(o);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) attn_ld32(s_at + 32 * c, s + 32 * c);
-                attn_ld_wait(s);
-                float sc = a.scale_log2;
-                if (key0 + kAttnTile > clear || there != all) {
-                    const int to_lim = lim - key0, to_ctx = q.ctx - key0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t see = attn_prefix(to_lim, j);
-                        if (PAGED) {
-                            if (tree) {
-                                const int up = to_ctx - 32 * j;
-                                const uint32_t nodes = up >= 32 || up <= -64 ? 0u : up >= 0 ? (uint32_t)(anc << up) : (uint32_t)(anc >> -up);
-                                see &= attn_prefix(to_ctx, j) | nodes;
+                                for (int j = 0; j < 32; ++j) o[j] *= f;
+                                tc_st16(o_at + 32 * c, reinterpret_cast<uint32_t(&)[16]>(o[0]));
+                                tc_st16(o_at + 32 * c + 16, reinterpret_cast<uint32_t(&)[16]>(o[16]));
                             }
-                            if (a.page_shift == 4)
-                                see &= ((there >> (2 * j)) & 1u ? 0xffffu : 0u) | ((there >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
-                            else
-                                see &= (there >> ((32 * j) >> a.page_shift)) & 1u ? ~0u : 0u;
-                        }
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) s[32 * j + c] = (see >> c) & 1u ? s[32 * j + c] * sc : -CUDART_INF_F;
-                    }
-                    sc = 1.f;
-                }
-                float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-                for (int c = 0; c < kAttnTile; c += 8)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) mx[j] = fmaxf(fmaxf(mx[j], s[c + 2 * j]), s[c + 2 * j + 1]);
-                float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                top = top == -CUDART_INF_F ? top : top * sc;
-                const bool move = top > m + kAttnSlack || (m == -CUDART_INF_F && top > m);
-                if (__any_sync(0xffffffffu, move)) {
-                    const float f = move ? exp2f(m - top) : 1.f;   // m = -inf: 0
-                    if (move) m = top;
-                    l *= f;
-                    if (i > 0) {                                  // the product before this tile has ended: S came behind it
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            float o[32];
-                            attn_ld32(o_at + 32 * c, o);
-                            attn_ld_wait(o);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) o[j] *= f;
-                            tc_st16(o_at + 32 * c, reinterpret_cast<uint32_t(&)[16]>(o[0]));
-                            tc_st16(o_at + 32 * c + 16, reinterpret_cast<uint32_t(&)[16]>(o[16]));
                         }
                     }
-                }
-                const float base = m == -CUDART_INF_F ? 0.f : m;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    return m == -CUDART_INF_F ? 0.f : m;
+                };
+                auto hand_over = [&](uint64_t *bar) {             // the weights written so far, to the matrix instructions
+                    attn_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar);
+                };
+                const bool masked = key0 + kAttnTile > clear || there != all;
+                if (PAIR && !masked) {
+                    // the row in registers: one pass over S
+                    float s[kAttnTile];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t pk[16];
+                    for (int c = 0; c < 4; ++c) attn_ld32(s_at + 32 * c, s + 32 * c);
+                    attn_ld_wait(s);
+                    float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float x = exp2f(fmaf(s[32 * c + 2 * j], sc, -base)), y = exp2f(fmaf(s[32 * c + 2 * j + 1], sc, -base));
-                        sum[j & 3] += x + y;
-                        const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
-                        pk[j] = reinterpret_cast<const uint32_t &>(b);
+                    for (int c = 0; c < kAttnTile; c += 8)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mx[j] = fmaxf(fmaxf(mx[j], s[c + 2 * j]), s[c + 2 * j + 1]);
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    const float sc = a.scale_log2, off = settle(top == -CUDART_INF_F ? top : top * sc);
+                    const float2 sc2 = make_float2(sc, sc), off2 = make_float2(-off, -off);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            float2 x = attn_fma2(make_float2(s[32 * c + 2 * j], s[32 * c + 2 * j + 1]), sc2, off2);
+                            if (j % 8 < kAttnPoly) {
+                                x = attn_exp2_poly(x);
+                            } else {
+                                x.x = exp2f(x.x);
+                                x.y = exp2f(x.y);
+                            }
+                            sum[j & 1] = attn_add2(sum[j & 1], x);
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(x.x, x.y);
+                            pk[j] = reinterpret_cast<const uint32_t &>(b);
+                        }
+                        tc_st16(s_at + 16 * c, pk);
+                        if (c == 1) hand_over(&p_half[w]);
                     }
-                    tc_st16(s_at + 16 * c, pk);
+                    sum[0] = attn_add2(sum[0], sum[1]);
+                    l += sum[0].x + sum[0].y;
+                } else {
+                    // Two passes over S, 32 columns at a time in a loop: a quarter of the instructions, which is what
+                    // counts where a call has few tiles (the first pass through code costs more than running it), and
+                    // where the time is that of reading the cache.
+                    const int to_lim = lim - key0, to_ctx = q.ctx - key0;
+                    const float sc = a.scale_log2;
+                    auto scaled = [&](int j, float (&s)[32]) {
+                        attn_ld32(s_at + 32 * j, s);
+                        attn_ld_wait(s);
+                        if (masked) {
+                            uint32_t see = attn_prefix(to_lim, j);
+                            if (PAGED) {
+                                if (tree) {
+                                    const int up = to_ctx - 32 * j;
+                                    const uint32_t nodes = up >= 32 || up <= -64 ? 0u : up >= 0 ? (uint32_t)(anc << up) : (uint32_t)(anc >> -up);
+                                    see &= attn_prefix(to_ctx, j) | nodes;
+                                }
+                                if (a.page_shift == 4)
+                                    see &= ((there >> (2 * j)) & 1u ? 0xffffu : 0u) | ((there >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
+                                else
+                                    see &= (there >> ((32 * j) >> a.page_shift)) & 1u ? ~0u : 0u;
+                            }
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) s[c] = (see >> c) & 1u ? s[c] * sc : -CUDART_INF_F;
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) s[c] *= sc;
+                        }
+                    };
+                    float top = -CUDART_INF_F, sum[2] = {0.f, 0.f};
+#pragma unroll 1
+                    for (int j = 0; j < 4; ++j) {
+                        float s[32];
+                        scaled(j, s);
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2) top = fmaxf(fmaxf(top, s[c]), s[c + 1]);
+                    }
+                    const float off = settle(top);
+#pragma unroll 1
+                    for (int j = 0; j < 4; ++j) {
+                        float s[32];
+                        uint32_t pk[16];
+                        scaled(j, s);
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) {
+                            const float x = exp2f(s[2 * c] - off), y = exp2f(s[2 * c + 1] - off);
+                            sum[c & 1] += x + y;
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+                            pk[c] = reinterpret_cast<const uint32_t &>(b);
+                        }
+                        tc_st16(s_at + 16 * j, pk);               // columns that this loop has read already
+                    }
+                    l += sum[0] + sum[1];
+                    hand_over(&p_half[w]);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                attn_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[w]);
+                hand_over(&p_full[w]);
             }
             if (n > 0) {                                          // the last product
                 wait(&s_full[w], s_phase);
@@ -405,6 +555,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 tc_fence_after();
             }
             r0 += p.t1 - p.t0;
+            ++pieces;
             float f[2] = {1.f, 0.f};
             bool two = false;
             if (!PAIR) {
@@ -430,7 +581,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 const long long at = (long long)p.slot * a.rows_tile + (PAIR ? w * half : 0) + row_in;
                 float *dst_p = a.part_o + at * D + col0;
                 __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.out) + ((long long)(q.tok0 + token) * a.Hk * a.group + head) * D + col0;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < CW / 32; ++c) {
                     float o[32];
                     attn_ld32((PAIR ? o_at : tmem_o[0] + lanes) + col0 + 32 * c, o);
