@@ -7,7 +7,7 @@
 // memory for the whole item.  The running maximum is only moved when a row's maximum grows by more than 2^8: until then
 // weights are at most 2^8, and O need not be read and scaled.
 //
-// Roles: two groups of four softmax warps, one warp that issues the matrix instructions, one that issues the copies.
+// Roles: two groups of four softmax warps, a warp for each that issues its matrix instructions, one that issues the copies.
 // While one group is between its S and its P the tensor cores work for the other one:
 //   PAIR    the two groups hold 128 rows each of the same key/value head and share every tile (many rows)
 //   !PAIR   the two groups hold the same rows and take every other tile, their results are joined at the end (few rows:
@@ -27,8 +27,9 @@
 namespace s2moe {
 
 constexpr int kAttnTile = 128;
-constexpr int kAttnThreads = 384;                 // 8 softmax warps, matrix instructions, copies, two warps without work
+constexpr int kAttnThreads = 384;                 // 8 softmax warps, 2 for matrix instructions, 1 for copies, 1 without work
 constexpr int kAttnHalf = 128 * 128;              // bytes of 128 rows x 64 columns
+constexpr int kAttnPart = 3;                      // of 4 parts of a tile's weights, those handed over first
 constexpr int kAttnPoly = 2;                      // of 8 pairs of weights, those that take the polynomial
 constexpr float kAttnSlack = 8.f;                 // log2 of the largest weight before the maximum is moved
 
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     using Iter = AttnIter<PAGED, SPLIT, kAttnTile>;
     constexpr int NS = L::slots;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], p_half[2], p_full[2], ended, n_full[2], n_empty[2];
+    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], p_part[2], p_full[2], ended[2], turn_of[2], n_full[2], n_empty[2];
     __shared__ __align__(16) uint4 next_cta[2];
     __shared__ uint32_t tmem_at;
     __shared__ float2 ml[2][128];
@@ -131,17 +132,18 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) {
             mbar_init(&full[i], 1);
-            mbar_init(&empty[i], 1);
+            mbar_init(&empty[i], PAIR ? 2 : 1);
         }
         mbar_init(&q_full, 1);
-        mbar_init(&q_empty, 1);
-        mbar_init(&ended, 1);
+        mbar_init(&q_empty, 2);
         for (int w = 0; w < 2; ++w) {
             mbar_init(&s_full[w], 1);
-            mbar_init(&p_half[w], 4);
+            mbar_init(&p_part[w], 4);
+            mbar_init(&ended[w], 1);
+            mbar_init(&turn_of[w], 1);
             mbar_init(&p_full[w], 4);
             mbar_init(&n_full[w], 1);
-            mbar_init(&n_empty[w], 10);
+            mbar_init(&n_empty[w], 11);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     unsigned pieces = 0;
     // Without a split the grid has a block per item, and a CTA that has an item under way takes the next block that has
     // not started yet over (the hardware's work queue: no counter in memory, and no CTA waits for its start-up again).
-    // The copying warp asks one item ahead; all ten working warps read the answer.
+    // The copying warp asks one item ahead; all eleven working warps read the answer.
     auto next = [&]() -> bool {
         if (SPLIT) return it.next(p);
         int unit = (int)blockIdx.x;
@@ -266,97 +268,101 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         // nothing may land in shared memory that is no longer this CTA's
         if (!ok)
             for (int i = 0; i < NS; ++i) mbar_wait(&full[i], 0), mbar_wait(&full[i], 1);
-    } else if (warp == 8) {
-        // ------------------------------------------------------------------ matrix instructions
+    } else if (warp != 11) {
+        // ------------------------------------------------------------------ matrix instructions: a warp per softmax group
+        // (one warp for both was the bound: with its waits and commits it took 1700 cycles per tile and group, the tensor
+        // cores need 1024)
+        const int w = warp == 10;
         const bool leader = tc_elect();
         // D = F32, A = B = BF16, M = 128; bit 16: B's rows (not its columns) are contiguous
         const uint32_t idesc_s = tc_idesc(kAttnTile), idesc_o = tc_idesc(D) | (1u << 16);
-        const uint64_t kd = tc_smem_desc(ring), qd = tc_smem_desc(qs);
+        const uint64_t kd = tc_smem_desc(ring), qd = tc_smem_desc(qs + (PAIR ? w * L::tile : 0));
         // V: 64-column blocks kAttnHalf apart, groups of 8 keys 1024 bytes apart
         const uint64_t vd = (kd & ~(0x3fffull << 16)) | ((uint64_t)(kAttnHalf >> 4) << 16);
-        const uint32_t k_hi = (uint32_t)(kd >> 32), v_hi = (uint32_t)(vd >> 32), q_hi = (uint32_t)(qd >> 32);
-        uint32_t p_phase[2] = {0, 0};
+        const uint32_t k_hi = (uint32_t)(kd >> 32), v_hi = (uint32_t)(vd >> 32), q_hi = (uint32_t)(qd >> 32), q_lo = (uint32_t)qd;
+        const uint32_t ts = w ? tmem_s[1] : tmem_s[0], to = w ? tmem_o[1] : tmem_o[0];
+        uint32_t p_phase = 0, turn = 0;
         while (next()) {
             if (leader && ok) {
-                const int n[2] = {tiles_of(p, 0), tiles_of(p, 1)}, nt = p.t1 - p.t0;
-                auto scores = [&](int w, int t) {                 // S of group w from tile t of the piece
-                    const unsigned c = 2 * (r0 + t), slot = c % NS;
+                const int n = tiles_of(p, w), nt = p.t1 - p.t0;
+                auto arrived = [&](int t, int kv) -> unsigned {   // slot of a tile of the piece, once it is there
+                    const unsigned c = 2 * (r0 + t) + kv, slot = c % NS;
                     wait(&full[slot], (c / NS) & 1u);
+                    return slot;
+                };
+                auto scores = [&](int t) {                        // S = Q K^T, then K's slot is free
+                    const unsigned slot = arrived(t, 0);
                     tc_fence_after();
-                    const uint32_t ql = (uint32_t)qd + (PAIR ? w * (L::tile >> 4) : 0), kl = (uint32_t)kd + slot * (L::tile >> 4);
+                    const uint32_t kl = (uint32_t)kd + slot * (L::tile >> 4);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t o = (k / 4) * (kAttnHalf >> 4) + (k % 4) * 2;
-                        tc_mma_bf16_parts(tmem_s[w], ql + o, q_hi, kl + o, k_hi, idesc_s, k > 0);
+                        tc_mma_bf16_parts(ts, q_lo + o, q_hi, kl + o, k_hi, idesc_s, k > 0);
                     }
+                    return slot;
                 };
-                auto product = [&](int w, int t, bool first) {    // O of group w from its weights and tile t
-                    const unsigned c = 2 * (r0 + t) + 1, slot = c % NS;
-                    wait(&full[slot], (c / NS) & 1u);
-                    wait(&p_half[w], p_phase[w]);
+                auto product = [&](int t, bool first) {           // O += P V
+                    const unsigned slot = arrived(t, 1);
+                    wait(&p_part[w], p_phase);
                     tc_fence_after();
                     const uint32_t vl = (uint32_t)vd + slot * (L::tile >> 4);
 #pragma unroll
                     for (int k = 0; k < kAttnTile / 16; ++k) {
-                        if (k == kAttnTile / 32) {
-                            wait(&p_full[w], p_phase[w]);
+                        if (k == 2 * kAttnPart) {
+                            wait(&p_full[w], p_phase);
                             tc_fence_after();
                         }
-                        tc_mma_bf16_tmem_a(tmem_o[w], tmem_s[w] + 8 * k, vl + k * 128, v_hi, idesc_o, !first || k > 0);
+                        tc_mma_bf16_tmem_a(to, ts + 8 * k, vl + k * 128, v_hi, idesc_o, !first || k > 0);
                     }
-                    p_phase[w] ^= 1u;
+                    p_phase ^= 1u;
+                    return slot;
                 };
-                auto release = [&](int t, int kv) { tc_commit(&empty[(2 * (r0 + t) + kv) % NS]); };
+                auto pass = [&](bool both) {
+                    if (!both) return;
+                    mbar_arrive(&turn_of[w ^ 1]);
+                    ++turn;
+                };
                 wait(&q_full, pieces & 1u);
-                if (PAIR) {
-                    for (int w = 0; w < 2; ++w)
-                        if (n[w] > 0) {
-                            scores(w, 0);
-                            tc_commit(&s_full[w]);
-                        }
-                    release(0, 0);
-                    if (nt == 1) tc_commit(&q_empty);
-                    for (int t = 0; t < nt && ok; ++t) {
-                        for (int w = 0; w < 2; ++w) {
-                            if (t >= n[w]) continue;
-                            const bool last = w == 1 || t >= n[1], last_k = w == 1 || t + 1 >= n[1];
-                            product(w, t, t == 0);
-                            if (last) release(t, 1);
-                            if (t + 1 < n[w]) {
-                                scores(w, t + 1);
-                                if (last_k) release(t + 1, 0);
-                                if (last_k && t + 2 == nt) tc_commit(&q_empty);
-                            }
-                            tc_commit(&s_full[w]);
-                        }
-                    }
-                } else {
-                    for (int w = 0; w < 2 && w < nt; ++w) {
-                        scores(w, w);
-                        release(w, 0);
+                // PAIR: a slot is free when both groups are through with it; one that has no use for a tile says so
+                const int step = PAIR ? 1 : 2, t_end = PAIR ? n : nt;
+                int t = PAIR ? 0 : w;
+                if (t < t_end) {
+                    const unsigned slot = scores(t);
+                    tc_commit(&s_full[w]);
+                    tc_commit(&empty[slot]);
+                }
+                if (t + step >= t_end) tc_commit(&q_empty);
+                // Tiles that both groups take go through the tensor cores group by group: handed in at the same time they
+                // would end at the same time, and then both groups would be between S and P together, with the tensor
+                // cores idle and one set of units for exponentials between them.
+                const int turns = PAIR && tiles_of(p, 1) > 0 ? tiles_of(p, 0) : 0;
+                for (; t < t_end && ok; t += step) {
+                    if (t < turns && (w == 1 || turn > 0)) wait(&turn_of[w], (w == 1 ? turn : turn - 1) & 1u);
+                    const unsigned vslot = product(t, t < step);
+                    if (t + step < t_end) {
+                        const unsigned kslot = scores(t + step);
+                        pass(t < turns);
                         tc_commit(&s_full[w]);
-                    }
-                    if (nt <= 2) tc_commit(&q_empty);
-                    for (int t = 0; t < nt && ok; ++t) {
-                        const int w = t & 1;
-                        product(w, t, t < 2);
-                        release(t, 1);
-                        if (t + 2 < nt) {
-                            scores(w, t + 2);
-                            release(t + 2, 0);
-                            if (t + 3 == nt) tc_commit(&q_empty);
-                        }
+                        tc_commit(&empty[vslot]);
+                        tc_commit(&empty[kslot]);
+                        if (t + 2 * step >= t_end) tc_commit(&q_empty);
+                    } else {
+                        pass(t < turns);
                         tc_commit(&s_full[w]);
+                        tc_commit(&empty[vslot]);
                     }
                 }
+                if (PAIR)
+                    for (; t < nt && ok; ++t)
+                        for (int kv = 0; kv < 2; ++kv) mbar_arrive(&empty[arrived(t, kv)]);
             }
             __syncwarp();
             r0 += p.t1 - p.t0;
             ++pieces;
         }
         if (leader && !ok) {                                      // no instruction outlives the CTA's tensor memory
-            tc_commit(&ended);
-            mbar_wait(&ended, 0);
+            tc_commit(&ended[w]);
+            mbar_wait(&ended[w], 0);
         }
         __syncwarp();
     }
@@ -422,7 +428,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive(&p_half[w]);
+                        mbar_arrive(&p_part[w]);
                         mbar_arrive(&p_full[w]);
                     }
                     continue;
@@ -488,7 +494,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                             pk[j] = reinterpret_cast<const uint32_t &>(b);
                         }
                         tc_st16(s_at + 16 * c, pk);
-                        if (c == 1) hand_over(&p_half[w]);
+                        if (c == kAttnPart - 1) hand_over(&p_part[w]);
                     }
                     sum[0] = attn_add2(sum[0], sum[1]);
                     l += sum[0].x + sum[0].y;
@@ -545,7 +551,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         tc_st16(s_at + 16 * j, pk);               // columns that this loop has read already
                     }
                     l += sum[0] + sum[1];
-                    hand_over(&p_half[w]);
+                    hand_over(&p_part[w]);
                 }
                 hand_over(&p_full[w]);
             }
