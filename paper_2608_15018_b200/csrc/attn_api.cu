@@ -175,6 +175,10 @@ int launch(int64_t grid, int threads, size_t smem, cudaStream_t st, bool behind,
     return cudaLaunchKernelEx(&lc, Kernel, args...) == cudaSuccess ? S2MOE_OK : S2MOE_ECUDA;
 }
 
+// Exponentials are taken to base 2.  A scale of 0 (all weights alike) would make NaN of the -infinity of an unseen key;
+// at 1e-30 every weight is 1 as well.
+float scale_log2(float scale) { return scale < 1e-30f ? 1e-30f : scale * 1.44269504f; }
+
 int64_t grid_for(int64_t items) { return items < (1 << 20) ? items : 1 << 20; }
 
 template <int D, int R, bool PAGED, bool SPLIT>
@@ -257,7 +261,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     a.seq_start = seq_start;
     a.n_seq = n_seq; a.n_tokens = a.n_nodes = n_tokens; a.Hk = n_kv_heads; a.group = n_heads / n_kv_heads;
     a.min_units = 1;
-    a.scale_log2 = scale * 1.44269504f;
+    a.scale_log2 = scale_log2(scale);
     const DeviceFacts *facts = device_facts();
     if (!facts) return S2MOE_ECUDA;
     a.status = facts->status;
@@ -316,7 +320,7 @@ int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_s
     a.n_seq = n_seq; a.n_tokens = n_tokens; a.n_nodes = n_nodes;
     a.Hk = cache->n_kv_heads; a.group = n_heads / cache->n_kv_heads;
     a.table_width = table_width; a.page_shift = page_shift(cache->page_size); a.n_pages = cache->n_pages;
-    a.scale_log2 = scale * 1.44269504f;
+    a.scale_log2 = scale_log2(scale);
     a.part_o = (float *)workspace;
     a.part_ml = (float *)workspace + (int64_t)p.grid * 2 * p.rows_tile * cache->head_dim;
     a.status = facts->status;

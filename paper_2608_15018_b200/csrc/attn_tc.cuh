@@ -30,7 +30,6 @@ constexpr int kAttnTile = 128;
 constexpr int kAttnThreads = 384;                 // 8 softmax warps, 2 for matrix instructions, 1 for copies, 1 without work
 constexpr int kAttnHalf = 128 * 128;              // bytes of 128 rows x 64 columns
 constexpr int kAttnPart = 3;                      // of 4 parts of a tile's weights, those handed over first
-constexpr int kAttnPoly = 2;                      // of 8 pairs of weights, those that take the polynomial
 constexpr float kAttnSlack = 8.f;                 // log2 of the largest weight before the maximum is moved
 
 template <int D, bool PAIR>
@@ -82,29 +81,23 @@ __device__ __forceinline__ float2 attn_add2(float2 x, float2 y)
     asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
     return r;
 }
-__device__ __forceinline__ float2 attn_mul2(float2 x, float2 y)
-{
-    float2 r;
-    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
-    return r;
-}
 
-// 2^x for two x <= 64 on the multiply-add pipe: x = n + r with n the nearest integer, 2^r for |r| <= 1/2 by a polynomial of
-// degree 4 (fitted for the smallest largest relative error, 2.7e-6 with its coefficients in binary32), 2^n put together as
-// a number.  x below -126 counts as -126, NaN stays NaN.
-__device__ __forceinline__ float2 attn_exp2_poly(float2 x)
+// 4 x 4 transposition of 16-byte pieces among four neighbouring lanes: lane i's piece j becomes lane j's piece i
+__device__ __forceinline__ void attn_swap4(uint32_t (&u)[16], int lane)
 {
-    constexpr float kMagic = 12582912.f + 127.f;                  // 1.5 * 2^23: the sum's low bits are n + 127
-    asm("max.NaN.ftz.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-    asm("max.NaN.ftz.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-    const float2 t = attn_add2(x, make_float2(kMagic, kMagic));
-    const float2 n = attn_add2(t, make_float2(-kMagic, -kMagic));
-    const float2 r = attn_fma2(n, make_float2(-1.f, -1.f), x);
-    float2 y = attn_fma2(r, make_float2(0.009570102f, 0.009570102f), make_float2(0.055917859f, 0.055917859f));
-    y = attn_fma2(y, r, make_float2(0.24024744f, 0.24024744f));
-    y = attn_fma2(y, r, make_float2(0.69312179f, 0.69312179f));
-    y = attn_fma2(y, r, make_float2(0.99999928f, 0.99999928f));
-    return attn_mul2(y, make_float2(__uint_as_float(__float_as_uint(t.x) << 23), __uint_as_float(__float_as_uint(t.y) << 23)));
+#pragma unroll
+    for (int m = 1; m <= 2; ++m)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int j = m == 1 ? 2 * k : k, j2 = j + m;
+            const bool odd = (lane & m) != 0;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? u[4 * j + x] : u[4 * j2 + x], m);
+                if (odd) u[4 * j + x] = got;
+                else u[4 * j2 + x] = got;
+            }
+        }
 }
 
 // bits [0, n) of a word whose bits stand for keys from 32 * j on
@@ -121,7 +114,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     using Iter = AttnIter<PAGED, SPLIT, kAttnTile>;
     constexpr int NS = L::slots;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], p_part[2], p_full[2], ended[2], turn_of[2], n_full[2], n_empty[2];
+    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], o_full[2], p_part[2], p_full[2], ended[2], turn_of[2], n_full[2], n_empty[2];
     __shared__ __align__(16) uint4 next_cta[2];
     __shared__ uint32_t tmem_at;
     __shared__ float2 ml[2][128];
@@ -138,6 +131,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         mbar_init(&q_empty, 2);
         for (int w = 0; w < 2; ++w) {
             mbar_init(&s_full[w], 1);
+            mbar_init(&o_full[w], 1);
             mbar_init(&p_part[w], 4);
             mbar_init(&ended[w], 1);
             mbar_init(&turn_of[w], 1);
@@ -348,7 +342,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         if (t + 2 * step >= t_end) tc_commit(&q_empty);
                     } else {
                         pass(t < turns);
-                        tc_commit(&s_full[w]);
+                        // (a barrier of its own: the next item's first S may be there before this is waited for)
+                        tc_commit(&o_full[w]);
                         tc_commit(&empty[vslot]);
                     }
                 }
@@ -374,9 +369,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // this warp's 32 lanes of tensor memory
         const uint32_t s_at = tmem_s[w] + lanes, o_at = tmem_o[w] + lanes;
         const int ppt = PAGED ? kAttnTile >> a.page_shift : 0;
-        uint32_t s_phase = 0;
-        while (next()) {
-            const AttnSeq &q = p.q;
+        uint32_t s_phase = 0, o_phase = 0;
+        bool have_piece = next();
+        while (have_piece) {
+            const AttnPiece ahead = p, &at_hand = SPLIT ? p : ahead;
+            const AttnSeq &q = at_hand.q;
             const int n = tiles_of(p, w), row = p.rt * a.rows_tile + (PAIR ? w * half : 0) + row_in;
             const bool mine = row_in < half && row < q.n * a.group, used = __any_sync(0xffffffffu, mine);
             const int token = mine ? row / a.group : 0, head = p.h * a.group + (mine ? row % a.group : 0);
@@ -384,10 +381,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             const bool tree = PAGED && a.parent && !q.bad;
             unsigned long long anc = 0;
             bool have_anc = !tree;
-            // keys below this one every row of the warp sees
-            int clear = tree ? min(lim, q.ctx) : lim;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) clear = min(clear, __shfl_xor_sync(0xffffffffu, clear, o));
+            // keys below `clear` every row of the warp sees, keys from `reach` on none
+            const int clear = __reduce_min_sync(0xffffffffu, tree ? min(lim, q.ctx) : lim), reach = __reduce_max_sync(0xffffffffu, mine ? lim : 0);
             float m = -CUDART_INF_F, l = 0.f;                     // maximum in use (times scale_log2), sum of weights
             for (int i = 0; i < n; ++i) {
                 const int t = PAIR ? i : 2 * i + w, key0 = (p.t0 + t) * kAttnTile;
@@ -462,19 +457,38 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     if (lane == 0) mbar_arrive(bar);
                 };
                 const bool masked = key0 + kAttnTile > clear || there != all;
+                // which keys of 32 j .. 32 j + 31 of the tile the row sees
+                auto seen = [&](int j) -> uint32_t {
+                    uint32_t see = attn_prefix(lim - key0, j);
+                    if (PAGED) {
+                        if (tree) {
+                            const int up = q.ctx - key0 - 32 * j;
+                            const uint32_t nodes = up >= 32 || up <= -64 ? 0u : up >= 0 ? (uint32_t)(anc << up) : (uint32_t)(anc >> -up);
+                            see &= attn_prefix(up, 0) | nodes;
+                        }
+                        if (a.page_shift == 4)
+                            see &= ((there >> (2 * j)) & 1u ? 0xffffu : 0u) | ((there >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
+                        else
+                            see &= (there >> ((32 * j) >> a.page_shift)) & 1u ? ~0u : 0u;
+                    }
+                    return see;
+                };
+                const float sc = a.scale_log2;
                 if (PAIR && !masked) {
-                    // the row in registers: one pass over S
-                    float s[kAttnTile];
+                    // the row in registers: one pass over S (a part's maximum is taken while the next part is on its way)
+                    float s[4][32], mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                    attn_ld32(s_at, s[0]);
+                    attn_ld_wait(s[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) attn_ld32(s_at + 32 * c, s + 32 * c);
-                    attn_ld_wait(s);
-                    float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                    for (int c = 0; c < 4; ++c) {
+                        if (c < 3) attn_ld32(s_at + 32 * (c + 1), s[c + 1]);
 #pragma unroll
-                    for (int c = 0; c < kAttnTile; c += 8)
+                        for (int j = 0; j < 32; j += 8)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) mx[j] = fmaxf(fmaxf(mx[j], s[c + 2 * j]), s[c + 2 * j + 1]);
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                    const float sc = a.scale_log2, off = settle(top == -CUDART_INF_F ? top : top * sc);
+                            for (int x = 0; x < 4; ++x) mx[x] = fmaxf(fmaxf(mx[x], s[c][j + 2 * x]), s[c][j + 2 * x + 1]);
+                        if (c < 3) attn_ld_wait(s[c + 1]);
+                    }
+                    const float off = settle(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc);
                     const float2 sc2 = make_float2(sc, sc), off2 = make_float2(-off, -off);
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -482,13 +496,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         uint32_t pk[16];
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            float2 x = attn_fma2(make_float2(s[32 * c + 2 * j], s[32 * c + 2 * j + 1]), sc2, off2);
-                            if (j % 8 < kAttnPoly) {
-                                x = attn_exp2_poly(x);
-                            } else {
-                                x.x = exp2f(x.x);
-                                x.y = exp2f(x.y);
-                            }
+                            float2 x = attn_fma2(make_float2(s[c][2 * j], s[c][2 * j + 1]), sc2, off2);
+                            x.x = exp2f(x.x);
+                            x.y = exp2f(x.y);
                             sum[j & 1] = attn_add2(sum[j & 1], x);
                             const __nv_bfloat162 b = __floats2bfloat162_rn(x.x, x.y);
                             pk[j] = reinterpret_cast<const uint32_t &>(b);
@@ -501,49 +511,35 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 } else {
                     // Two passes over S, 32 columns at a time in a loop: a quarter of the instructions, which is what
                     // counts where a call has few tiles (the first pass through code costs more than running it), and
-                    // where the time is that of reading the cache.
-                    const int to_lim = lim - key0, to_ctx = q.ctx - key0;
-                    const float sc = a.scale_log2;
-                    auto scaled = [&](int j, float (&s)[32]) {
+                    // where the time is that of reading the cache.  Parts that no row of the warp sees (the upper triangle
+                    // of a prompt) are left out.
+                    const int parts = min(4, max(0, (reach - key0 + 31) / 32));
+                    auto part_of = [&](int j, float (&s)[32]) {
                         attn_ld32(s_at + 32 * j, s);
                         attn_ld_wait(s);
                         if (masked) {
-                            uint32_t see = attn_prefix(to_lim, j);
-                            if (PAGED) {
-                                if (tree) {
-                                    const int up = to_ctx - 32 * j;
-                                    const uint32_t nodes = up >= 32 || up <= -64 ? 0u : up >= 0 ? (uint32_t)(anc << up) : (uint32_t)(anc >> -up);
-                                    see &= attn_prefix(to_ctx, j) | nodes;
-                                }
-                                if (a.page_shift == 4)
-                                    see &= ((there >> (2 * j)) & 1u ? 0xffffu : 0u) | ((there >> (2 * j + 1)) & 1u ? 0xffff0000u : 0u);
-                                else
-                                    see &= (there >> ((32 * j) >> a.page_shift)) & 1u ? ~0u : 0u;
-                            }
+                            const uint32_t see = seen(j);
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) s[c] = (see >> c) & 1u ? s[c] * sc : -CUDART_INF_F;
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) s[c] *= sc;
+                            for (int c = 0; c < 32; ++c) s[c] = (see >> c) & 1u ? s[c] : -CUDART_INF_F;
                         }
                     };
                     float top = -CUDART_INF_F, sum[2] = {0.f, 0.f};
 #pragma unroll 1
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < parts; ++j) {
                         float s[32];
-                        scaled(j, s);
+                        part_of(j, s);
 #pragma unroll
                         for (int c = 0; c < 32; c += 2) top = fmaxf(fmaxf(top, s[c]), s[c + 1]);
                     }
-                    const float off = settle(top);
+                    const float off = settle(top * sc);
 #pragma unroll 1
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < parts; ++j) {
                         float s[32];
                         uint32_t pk[16];
-                        scaled(j, s);
+                        part_of(j, s);
 #pragma unroll
                         for (int c = 0; c < 16; ++c) {
-                            const float x = exp2f(s[2 * c] - off), y = exp2f(s[2 * c + 1] - off);
+                            const float x = exp2f(fmaf(s[2 * c], sc, -off)), y = exp2f(fmaf(s[2 * c + 1], sc, -off));
                             sum[c & 1] += x + y;
                             const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
                             pk[c] = reinterpret_cast<const uint32_t &>(b);
@@ -551,17 +547,25 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         tc_st16(s_at + 16 * j, pk);               // columns that this loop has read already
                     }
                     l += sum[0] + sum[1];
+#pragma unroll 1
+                    for (int j = parts; j < 4; ++j) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) pk[c] = 0u;
+                        tc_st16(s_at + 16 * j, pk);
+                    }
                     hand_over(&p_part[w]);
                 }
                 hand_over(&p_full[w]);
             }
-            if (n > 0) {                                          // the last product
-                wait(&s_full[w], s_phase);
-                s_phase ^= 1u;
-                tc_fence_after();
-            }
             r0 += p.t1 - p.t0;
             ++pieces;
+            if (!SPLIT) have_piece = next();                      // while the last product is under way
+            if (n > 0) {
+                wait(&o_full[w], o_phase);
+                o_phase ^= 1u;
+                tc_fence_after();
+            }
             float f[2] = {1.f, 0.f};
             bool two = false;
             if (!PAIR) {
@@ -570,7 +574,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 tc_fence_after();
                 const float2 x = ml[0][row_in], y = ml[1][row_in];
-                two = p.t1 - p.t0 > 1;
+                two = at_hand.t1 - at_hand.t0 > 1;
                 m = fmaxf(x.x, y.x);
                 const float b = m == -CUDART_INF_F ? 0.f : m;
                 f[0] = exp2f(x.x - b);
@@ -580,13 +584,26 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             // the columns this thread writes, 32 at a time
             constexpr int CW = PAIR ? D : D / 2;
             const int col0 = PAIR ? 0 : w * CW;
-            const bool part = SPLIT && p.slot >= 0;
+            const bool part = SPLIT && at_hand.slot >= 0;
             const float inv = part ? 1.f : q.bad ? CUDART_NAN_F : 1.f / l;
             bool fine = true;
             if (used) {
-                const long long at = (long long)p.slot * a.rows_tile + (PAIR ? w * half : 0) + row_in;
-                float *dst_p = a.part_o + at * D + col0;
-                __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.out) + ((long long)(q.tok0 + token) * a.Hk * a.group + head) * D + col0;
+                const long long at = (long long)at_hand.slot * a.rows_tile + (PAIR ? w * half : 0) + row_in;
+                // A thread has a row, but 32 lanes that each write 16 bytes of another row cost 32 accesses: four neighbours
+                // swap pieces, so that they write 64 bytes of each of their rows together.
+                uint8_t *dst = part ? reinterpret_cast<uint8_t *>(a.part_o + at * D + col0)
+                                    : reinterpret_cast<uint8_t *>(reinterpret_cast<__nv_bfloat16 *>(a.out) +
+                                                                  ((long long)(q.tok0 + token) * a.Hk * a.group + head) * D + col0);
+                uint8_t *rows[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    rows[j] = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, mine ? reinterpret_cast<unsigned long long>(dst) : 0ull, (lane & ~3) + j));
+                auto put = [&](uint32_t (&u)[16], int at_byte) {
+                    attn_swap4(u, lane);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (rows[j]) *reinterpret_cast<uint4 *>(rows[j] + at_byte + 16 * (lane & 3)) = make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
+                };
 #pragma unroll 1
                 for (int c = 0; c < CW / 32; ++c) {
                     float o[32];
@@ -605,22 +622,23 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     } else {
                         attn_ld_wait(o);
                     }
-                    if (mine && part) {
+                    uint32_t u[16];
+                    if (part) {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) attn_store4(dst_p + 32 * c + j, make_float4(o[j], o[j + 1], o[j + 2], o[j + 3]));
-                    } else if (mine) {
+                        for (int k = 0; k < 2; ++k) {
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            uint32_t u[4];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) {
-                                const float y0 = o[j + 2 * x] * inv, y1 = o[j + 2 * x + 1] * inv;
-                                fine = fine && attn_finite(y0) && attn_finite(y1);
-                                const __nv_bfloat162 b = __floats2bfloat162_rn(y0, y1);
-                                u[x] = reinterpret_cast<const uint32_t &>(b);
-                            }
-                            *reinterpret_cast<uint4 *>(dst + 32 * c + j) = make_uint4(u[0], u[1], u[2], u[3]);
+                            for (int j = 0; j < 16; ++j) u[j] = __float_as_uint(o[16 * k + j]);
+                            put(u, 128 * c + 64 * k);
                         }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const float y0 = o[2 * j] * inv, y1 = o[2 * j + 1] * inv;
+                            fine = fine && attn_finite(y0) && attn_finite(y1);
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(y0, y1);
+                            u[j] = reinterpret_cast<const uint32_t &>(b);
+                        }
+                        put(u, 64 * c);
                     }
                 }
                 if (mine && part && (PAIR || w == 0)) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, l);
@@ -630,9 +648,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 tc_fence_after();
             }
+            __syncwarp();
             const unsigned again = __ballot_sync(0xffffffffu, mine && !part && !q.bad && !fine);
             if (again)
-                attn_fix_rows<__nv_bfloat16, D, PAGED>(a, q, p.s, p.h, again, token, head, p.t1 * kAttnTile, l == 0.f, col0, col0 + CW);
+                attn_fix_rows<__nv_bfloat16, D, PAGED>(a, q, at_hand.s, at_hand.h, again, token, head, at_hand.t1 * kAttnTile, l == 0.f, col0, col0 + CW);
+            if (SPLIT) have_piece = next();                       // (held early it costs registers, and a CTA has few pieces)
         }
     }
     tc_fence_before();
