@@ -7,7 +7,8 @@
 // memory for the whole item.  The running maximum is only moved when a row's maximum grows by more than 2^8: until then
 // weights are at most 2^8, and O need not be read and scaled.
 //
-// Roles: two groups of four softmax warps, a warp for each that issues its matrix instructions, one that issues the copies.
+// Roles: two groups of four softmax warps, a warp for each that issues its matrix instructions, a warp for the copies of
+// keys and values, which also finds the work, and one for those of q.
 // While one group is between its S and its P the tensor cores work for the other one:
 //   PAIR    the two groups hold 128 rows each of the same key/value head and share every tile (many rows)
 //   !PAIR   the two groups hold the same rows and take every other tile, their results are joined at the end (few rows:
@@ -27,7 +28,7 @@
 namespace s2moe {
 
 constexpr int kAttnTile = 128;
-constexpr int kAttnThreads = 384;                 // 8 softmax warps, 2 for matrix instructions, 1 for copies, 1 without work
+constexpr int kAttnThreads = 384;                 // 8 softmax warps, 2 for matrix instructions, 2 for copies
 constexpr int kAttnHalf = 128 * 128;              // bytes of 128 rows x 64 columns
 constexpr int kAttnPart = 3;                      // of 4 parts of a tile's weights, those handed over first
 constexpr float kAttnSlack = 8.f;                 // log2 of the largest weight before the maximum is moved
@@ -82,6 +83,13 @@ __device__ __forceinline__ float2 attn_add2(float2 x, float2 y)
     return r;
 }
 
+__device__ __forceinline__ float2 attn_mul2(float2 x, float2 y)
+{
+    float2 r;
+    asm("mul.rn.ftz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(r)) : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
+    return r;
+}
+
 // 4 x 4 transposition of 16-byte pieces among four neighbouring lanes: lane i's piece j becomes lane j's piece i
 __device__ __forceinline__ void attn_swap4(uint32_t (&u)[16], int lane)
 {
@@ -114,8 +122,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     using Iter = AttnIter<PAGED, SPLIT, kAttnTile>;
     constexpr int NS = L::slots;
     extern __shared__ uint8_t attn_raw[];
-    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full, q_empty, s_full[2], o_full[2], p_part[2], p_full[2], ended[2], turn_of[2], n_full[2], n_empty[2];
-    __shared__ __align__(16) uint4 next_cta[2];
+    __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2], o_full[2], p_part[2], p_full[2], ended[2], turn_of[2], n_full[2], n_empty[2], taken;
+    __shared__ __align__(16) uint4 next_cta;
+    __shared__ AttnPiece piece[2];                                // what the copying warp has found, one piece ahead
     __shared__ uint32_t tmem_at;
     __shared__ float2 ml[2][128];
     uint8_t *qs = attn_raw + ((1024u - (smem_u32(attn_raw) & 1023u)) & 1023u), *ring = qs + L::q;
@@ -127,9 +136,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], PAIR ? 2 : 1);
         }
-        mbar_init(&q_full, 1);
-        mbar_init(&q_empty, 2);
+        mbar_init(&taken, 1);
         for (int w = 0; w < 2; ++w) {
+            mbar_init(&q_full[w], 1);
+            mbar_init(&q_empty[w], PAIR ? 1 : 2);
             mbar_init(&s_full[w], 1);
             mbar_init(&o_full[w], 1);
             mbar_init(&p_part[w], 4);
@@ -156,79 +166,81 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             atomicExch(a.status, ST_MBAR_TIMEOUT);
         }
     };
+    // a block's tokens: rows_tile and half are multiples of the group
+    const int tok_block = a.rows_tile / a.group, tok_half = half / a.group;
     // tiles of each softmax group: PAIR: the first n of the item's, else every other one
     auto tiles_of = [&](const AttnPiece &p, int w) -> int {
         const int nt = p.t1 - p.t0;
         if (!PAIR) return (nt + 1 - w) / 2;
-        const int row = p.rt * a.rows_tile + w * half;
-        if (row >= p.q.n * a.group) return 0;
+        const int first_tok = p.rt * tok_block + w * tok_half;
+        if (first_tok >= p.q.n) return 0;
         if (PAGED || w == 1) return nt;
-        const int last = min(p.q.n, (row + half) / a.group) - 1;
+        const int last = min(p.q.n, first_tok + tok_half) - 1;
         return min(nt, (attn_limit<PAGED>(p.q, last) + kAttnTile - 1) / kAttnTile);
     };
     // A softmax thread holds a row of S (128 registers).  The launch gives 384 threads 168 registers each; moved about, 128
     // threads keep 72 and 256 have 216, which is the same sum.
-    Iter it(a, lane);
     AttnPiece p;
-    unsigned r0 = 0;                                              // tiles of the pieces before
-    unsigned pieces = 0;
-    // Without a split the grid has a block per item, and a CTA that has an item under way takes the next block that has
-    // not started yet over (the hardware's work queue: no counter in memory, and no CTA waits for its start-up again).
-    // The copying warp asks one item ahead; all eleven working warps read the answer.
+    unsigned r0 = 0, pieces = 0;                                  // tiles and pieces before this one
+    // The copying warp looks for the pieces and is ahead of the others by what the ring holds; they read what it found.
     auto next = [&]() -> bool {
-        if (SPLIT) return it.next(p);
-        int unit = (int)blockIdx.x;
-        if (pieces > 0) {
-            const unsigned k = pieces - 1, b = k & 1u;
-            wait(&n_full[b], (k >> 1) & 1u);
-            uint32_t got, x;
-            asm volatile(
-                "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
-                "ld.shared.b128 r, [%2];\n\t"
-                "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
-                "selp.u32 %0, 1, 0, p;\n\t"
-                "mov.u32 %1, 0;\n\t"
-                "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
-                : "=r"(got), "=r"(x)
-                : "r"(smem_u32(&next_cta[b]))
-                : "memory");
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&n_empty[b]);
-            if (!got || !__all_sync(0xffffffffu, ok)) return false;
-            unit = (int)x;
-        }
-        return it.item(unit, p);
+        const unsigned b = pieces & 1u;
+        wait(&n_full[b], (pieces >> 1) & 1u);
+        p = piece[b];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&n_empty[b]);
+        return p.t1 > 0 && __all_sync(0xffffffffu, ok);
     };
-
     if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    it.begin();
     if (warp == 9) {
-        // ------------------------------------------------------------------ copies
+        // ------------------------------------------------------------------ pieces and copies
         const int ppt = PAGED ? kAttnTile >> a.page_shift : 1;
-        while (next() && __all_sync(0xffffffffu, ok)) {
-            const int nw = PAIR && p.rt * a.rows_tile + half < p.q.n * a.group ? 2 : 1;
-            if (!SPLIT) {                                         // the item after this one
-                const unsigned b = pieces & 1u;
-                wait(&n_empty[b], ((pieces >> 1) & 1u) ^ 1u);
-                if (lane == 0 && ok) {
-                    mbar_expect_tx(&n_full[b], 16);
-                    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
-                                     smem_u32(&next_cta[b])),
-                                 "r"(smem_u32(&n_full[b]))
-                                 : "memory");
-                }
+        Iter it(a, lane);
+        it.begin();
+        // Without a split the grid has a block per item, and a CTA that has an item under way takes the next block that has
+        // not started yet over (the hardware's work queue: no counter in memory, and no CTA waits for its start-up again).
+        auto find = [&]() -> bool {
+            if (SPLIT) return it.next(p);
+            int unit = (int)blockIdx.x;
+            if (pieces > 0) {
+                wait(&taken, (pieces - 1) & 1u);
+                uint32_t got, x;
+                asm volatile(
+                    "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\t"
+                    "ld.shared.b128 r, [%2];\n\t"
+                    "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+                    "selp.u32 %0, 1, 0, p;\n\t"
+                    "mov.u32 %1, 0;\n\t"
+                    "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+                    : "=r"(got), "=r"(x)
+                    : "r"(smem_u32(&next_cta))
+                    : "memory");
+                fence_proxy_async();
+                __syncwarp();
+                if (!got || !__all_sync(0xffffffffu, ok)) return false;
+                unit = (int)x;
             }
-            wait(&q_empty, (pieces & 1u) ^ 1u);
+            if (!it.item(unit, p)) return false;
+            if (lane == 0) {                                      // the item after this one
+                mbar_expect_tx(&taken, 16);
+                asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                                 smem_u32(&next_cta)),
+                             "r"(smem_u32(&taken))
+                             : "memory");
+            }
+            return true;
+        };
+        for (bool more = true; more;) {
+            more = find();
+            const unsigned b = pieces & 1u;
+            wait(&n_empty[b], ((pieces >> 1) & 1u) ^ 1u);
             if (lane == 0) {
-                mbar_expect_tx(&q_full, (uint32_t)(nw * (D / 64) * half * 128));
-                for (int w = 0; w < nw; ++w)
-                    for (int c = 0; c < D / 64; ++c)
-                        tma_load_3d(qs + w * L::tile + c * kAttnHalf, &maps.q, 64 * c, p.h * a.group,
-                                    p.q.tok0 + (p.rt * a.rows_tile + w * half) / a.group, &q_full);
+                if (!more) p.t1 = 0;                              // the end
+                piece[b] = p;
+                mbar_arrive(&n_full[b]);
             }
-            __syncwarp();
+            if (!more || !__all_sync(0xffffffffu, ok)) break;
             for (int t = p.t0; t < p.t1 && __all_sync(0xffffffffu, ok); ++t) {
                 int x = 0;                                        // this lane's page, as the tensor's last coordinate
                 if (PAGED && lane < ppt) {
@@ -260,9 +272,29 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             ++pieces;
         }
         // nothing may land in shared memory that is no longer this CTA's
-        if (!ok)
+        if (!ok) {
             for (int i = 0; i < NS; ++i) mbar_wait(&full[i], 0), mbar_wait(&full[i], 1);
-    } else if (warp != 11) {
+            mbar_wait(&taken, 0), mbar_wait(&taken, 1);
+        }
+    } else if (warp == 11) {
+        // ------------------------------------------------------------------ copies of the rows of q
+        // (a warp of its own: they wait for the last scores of the piece before, which the copies of keys must not)
+        for (; next(); ++pieces) {
+            for (int w = 0; w < (PAIR ? 2 : 1); ++w) {            // (each group's rows as soon as that group is through)
+                const int tok = p.rt * tok_block + w * tok_half;
+                wait(&q_empty[w], (pieces & 1u) ^ 1u);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                if (lane == 0) {
+                    mbar_expect_tx(&q_full[w], (uint32_t)(tok < p.q.n ? (D / 64) * half * 128 : 0));
+                    for (int c = 0; c < D / 64 && tok < p.q.n; ++c)
+                        tma_load_3d(qs + w * L::tile + c * kAttnHalf, &maps.q, 64 * c, p.h * a.group, p.q.tok0 + tok, &q_full[w]);
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok)
+            for (int w = 0; w < 2; ++w) mbar_wait(&q_full[w], 0), mbar_wait(&q_full[w], 1);
+    } else {
         // ------------------------------------------------------------------ matrix instructions: a warp per softmax group
         // (one warp for both was the bound: with its waits and commits it took 1700 cycles per tile and group, the tensor
         // cores need 1024)
@@ -316,7 +348,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     mbar_arrive(&turn_of[w ^ 1]);
                     ++turn;
                 };
-                wait(&q_full, pieces & 1u);
+                wait(&q_full[PAIR ? w : 0], pieces & 1u);
                 // PAIR: a slot is free when both groups are through with it; one that has no use for a tile says so
                 const int step = PAIR ? 1 : 2, t_end = PAIR ? n : nt;
                 int t = PAIR ? 0 : w;
@@ -325,7 +357,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     tc_commit(&s_full[w]);
                     tc_commit(&empty[slot]);
                 }
-                if (t + step >= t_end) tc_commit(&q_empty);
+                if (t + step >= t_end) tc_commit(&q_empty[PAIR ? w : 0]);
                 // Tiles that both groups take go through the tensor cores group by group: handed in at the same time they
                 // would end at the same time, and then both groups would be between S and P together, with the tensor
                 // cores idle and one set of units for exponentials between them.
@@ -339,7 +371,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         tc_commit(&s_full[w]);
                         tc_commit(&empty[vslot]);
                         tc_commit(&empty[kslot]);
-                        if (t + 2 * step >= t_end) tc_commit(&q_empty);
+                        if (t + 2 * step >= t_end) tc_commit(&q_empty[PAIR ? w : 0]);
                     } else {
                         pass(t < turns);
                         // (a barrier of its own: the next item's first S may be there before this is waited for)
@@ -363,20 +395,17 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        it.begin();
         // ------------------------------------------------------------------ softmax: one thread per row
         const int w = warp >> 2, row_in = tid & 127;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;        // this warp's 32 lanes of tensor memory
         const uint32_t s_at = tmem_s[w] + lanes, o_at = tmem_o[w] + lanes;
         const int ppt = PAGED ? kAttnTile >> a.page_shift : 0;
         uint32_t s_phase = 0, o_phase = 0;
-        bool have_piece = next();
-        while (have_piece) {
-            const AttnPiece ahead = p, &at_hand = SPLIT ? p : ahead;
-            const AttnSeq &q = at_hand.q;
-            const int n = tiles_of(p, w), row = p.rt * a.rows_tile + (PAIR ? w * half : 0) + row_in;
-            const bool mine = row_in < half && row < q.n * a.group, used = __any_sync(0xffffffffu, mine);
-            const int token = mine ? row / a.group : 0, head = p.h * a.group + (mine ? row % a.group : 0);
+        const int tok_in = row_in / a.group, head_in = row_in - tok_in * a.group;
+        while (next()) {
+            const AttnSeq &q = p.q;
+            const int n = tiles_of(p, w), token = p.rt * tok_block + (PAIR ? w * tok_half : 0) + tok_in, head = p.h * a.group + head_in;
+            const bool mine = row_in < half && token < q.n, used = __any_sync(0xffffffffu, mine);
             const int lim = mine ? attn_limit<PAGED>(q, token) : q.total;
             const bool tree = PAGED && a.parent && !q.bad;
             unsigned long long anc = 0;
@@ -560,7 +589,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             }
             r0 += p.t1 - p.t0;
             ++pieces;
-            if (!SPLIT) have_piece = next();                      // while the last product is under way
             if (n > 0) {
                 wait(&o_full[w], o_phase);
                 o_phase ^= 1u;
@@ -574,7 +602,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 asm volatile("bar.sync 1, 256;" ::: "memory");
                 tc_fence_after();
                 const float2 x = ml[0][row_in], y = ml[1][row_in];
-                two = at_hand.t1 - at_hand.t0 > 1;
+                two = p.t1 - p.t0 > 1;
                 m = fmaxf(x.x, y.x);
                 const float b = m == -CUDART_INF_F ? 0.f : m;
                 f[0] = exp2f(x.x - b);
@@ -584,11 +612,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             // the columns this thread writes, 32 at a time
             constexpr int CW = PAIR ? D : D / 2;
             const int col0 = PAIR ? 0 : w * CW;
-            const bool part = SPLIT && at_hand.slot >= 0;
+            const bool part = SPLIT && p.slot >= 0;
             const float inv = part ? 1.f : q.bad ? CUDART_NAN_F : 1.f / l;
-            bool fine = true;
+            float2 zero = make_float2(0.f, 0.f);
             if (used) {
-                const long long at = (long long)at_hand.slot * a.rows_tile + (PAIR ? w * half : 0) + row_in;
+                const long long at = (long long)p.slot * a.rows_tile + (PAIR ? w * half : 0) + row_in;
                 // A thread has a row, but 32 lanes that each write 16 bytes of another row cost 32 accesses: four neighbours
                 // swap pieces, so that they write 64 bytes of each of their rows together.
                 uint8_t *dst = part ? reinterpret_cast<uint8_t *>(a.part_o + at * D + col0)
@@ -633,9 +661,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     } else {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            const float y0 = o[2 * j] * inv, y1 = o[2 * j + 1] * inv;
-                            fine = fine && attn_finite(y0) && attn_finite(y1);
-                            const __nv_bfloat162 b = __floats2bfloat162_rn(y0, y1);
+                            const float2 y = attn_mul2(make_float2(o[2 * j], o[2 * j + 1]), make_float2(inv, inv));
+                            zero = attn_fma2(y, make_float2(0.f, 0.f), zero);      // NaN once a value is not finite
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
                             u[j] = reinterpret_cast<const uint32_t &>(b);
                         }
                         put(u, 64 * c);
@@ -649,10 +677,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 tc_fence_after();
             }
             __syncwarp();
-            const unsigned again = __ballot_sync(0xffffffffu, mine && !part && !q.bad && !fine);
+            const unsigned again = __ballot_sync(0xffffffffu, mine && !part && !q.bad && !(zero.x + zero.y == 0.f));
             if (again)
-                attn_fix_rows<__nv_bfloat16, D, PAGED>(a, q, at_hand.s, at_hand.h, again, token, head, at_hand.t1 * kAttnTile, l == 0.f, col0, col0 + CW);
-            if (SPLIT) have_piece = next();                       // (held early it costs registers, and a CTA has few pieces)
+                attn_fix_rows<__nv_bfloat16, D, PAGED>(a, q, p.s, p.h, again, token, head, p.t1 * kAttnTile, l == 0.f, col0, col0 + CW);
         }
     }
     tc_fence_before();
