@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import itertools
 import os
 from dataclasses import dataclass
@@ -537,13 +538,14 @@ def _int32(name: str, t: Optional[torch.Tensor], *shape: int) -> Optional[int]:
 
 def _rows(name: str, t: torch.Tensor, heads: int, dim: int, dtype: torch.dtype) -> Tuple[int, int]:
     """Address and token stride of [tokens][heads][dim] whose tokens may lie apart."""
-    if t.dtype is not dtype or t.dim() != 3 or t.shape[1:] != (heads, dim):
-        raise ValueError(f"{name}: {dtype} [tokens][{heads}][{dim}] expected, got {t.dtype} {list(t.shape)}")
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ValueError(f"{name}: {dtype} [tokens][{heads}][{dim}] expected, got {t.dtype} {list(shape)}")
     stride, address = heads * dim, t.data_ptr()
     if not t.is_contiguous():
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (t.size(0) > 1 and t.stride(0) < stride):
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim) or (shape[0] > 1 and t.stride(0) < stride):
             raise ValueError(f"{name}: the heads of a token must lie side by side, strides are {t.stride()}")
-        if t.size(0) > 1:
+        if shape[0] > 1:
             stride = t.stride(0)
     if address % 16 or stride * t.element_size() % 16:
         raise ValueError(f"{name}: tokens must start on 16-byte boundaries")
@@ -574,7 +576,7 @@ class KVCache:
             raise ValueError("k and v: float32 or bfloat16 [n_layers][n_pages][n_kv_heads][page_size][head_dim], alike")
         self.k, self.v = k, v
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device, self.index = k.dtype, k.device, k.get_device()
         self._c = KVCacheC(_dptr(k), _dptr(v), _DTYPES[k.dtype], *k.shape)
         self._ref = ctypes.byref(self._c)
 
@@ -596,7 +598,9 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_star
     if q.dim() != 3 or k.dim() != 3 or k.shape[0] != q.shape[0] or v.shape != k.shape or q.dtype not in _DTYPES:
         raise ValueError("q: float32 or bfloat16 [tokens][heads][dim]; k, v: [tokens][kv heads][dim]")
     n, heads, dim = q.shape
-    _on_device(q.device, k=k, v=v, seq_start=seq_start)
+    dev = _device()
+    if q.get_device() != dev or k.get_device() != dev or v.get_device() != dev or seq_start.get_device() != dev:
+        _on_device(q.device, k=k, v=v, seq_start=seq_start)
     qp, qs = _rows("q", q, heads, dim, q.dtype)
     kp, ks = _rows("k", k, k.shape[1], dim, q.dtype)
     vp, vs = _rows("v", v, k.shape[1], dim, q.dtype)
@@ -607,6 +611,18 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_star
     if rc != OK:
         raise S2MoEError(rc, "s2moe_prompt_attention")
     return out
+
+
+@functools.lru_cache(maxsize=512)
+def _tree_workspace(device: int, dtype: int, n_kv_heads: int, page_size: int, head_dim: int, n_seq: int, n_tokens: int, n_heads: int,
+                    table_width: int) -> int:
+    """Workspace of a tree attention call: a function of its sizes (and of the device's number of SMs)."""
+    cache = KVCacheC(16, 16, dtype, 1, 1, n_kv_heads, page_size, head_dim)       # (the addresses are not followed)
+    need = ctypes.c_int64(0)
+    rc = load_library().s2moe_tree_attention_workspace(ctypes.byref(cache), n_seq, n_tokens, n_heads, table_width, ctypes.byref(need))
+    if rc != OK:
+        raise S2MoEError(rc, "s2moe_tree_attention_workspace")
+    return need.value
 
 
 def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, page_table: torch.Tensor, context: torch.Tensor,
@@ -623,8 +639,12 @@ def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, page_table: torc
         raise ValueError("q: [tokens][heads][dim], page_table: [n_seq][width]")
     n, heads, dim = q.shape
     width = page_table.shape[1]
-    _on_device(q.device, cache=cache.k, page_table=page_table, context=context, seq_start=seq_start, parent=parent,
-               node_start=node_start)
+    dev = _device()
+    if (q.get_device() != dev or cache.index != dev or page_table.get_device() != dev or context.get_device() != dev
+            or seq_start.get_device() != dev or (parent is not None and parent.get_device() != dev)
+            or (node_start is not None and node_start.get_device() != dev)):
+        _on_device(q.device, cache=cache.k, page_table=page_table, context=context, seq_start=seq_start, parent=parent,
+                   node_start=node_start)
     if dim != cache.head_dim:
         raise ValueError(f"q has heads of {dim}, the cache of {cache.head_dim}")
     qp, qs = _rows("q", q, heads, dim, cache.dtype)
@@ -635,19 +655,17 @@ def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, page_table: torc
     starts, nodes = _int32("seq_start", seq_start, n_seq + 1), _int32("node_start", node_start, n_seq + 1)
     par = _int32("parent", parent, n_nodes)
     out = _output(out, q)
-    need = ctypes.c_int64(0)
-    rc = lib.s2moe_tree_attention_workspace(cache._ref, n_seq, n, heads, width, ctypes.byref(need))
-    if rc == OK:
-        ws = None
-        if need.value:
-            if stream is None:
-                ws = q.new_empty(need.value, dtype=torch.uint8)
-            else:
-                with torch.cuda.stream(stream):
-                    ws = q.new_empty(need.value, dtype=torch.uint8)
-        rc = lib.s2moe_tree_attention(cache._ref, int(layer), n_seq, n, heads, qp, qs, table, width, ctx, starts, n_nodes, nodes,
-                                      par, dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
-                                      None if ws is None else ws.data_ptr(), need.value, _stream_handle(stream))
+    need = _tree_workspace(dev, _DTYPES[cache.dtype], cache.n_kv_heads, cache.page_size, dim, n_seq, n, heads, width)
+    ws = None
+    if need:
+        if stream is None:
+            ws = q.new_empty(need, dtype=torch.uint8)
+        else:
+            with torch.cuda.stream(stream):
+                ws = q.new_empty(need, dtype=torch.uint8)
+    rc = lib.s2moe_tree_attention(cache._ref, int(layer), n_seq, n, heads, qp, qs, table, width, ctx, starts, n_nodes, nodes, par,
+                                  dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
+                                  None if ws is None else ws.data_ptr(), need, _stream_handle(stream))
     if rc != OK:
         raise S2MoEError(rc, "s2moe_tree_attention")
     return out
@@ -672,7 +690,10 @@ def kv_write(cache: KVCache, layer: int, k: torch.Tensor, v: torch.Tensor, page_
     if page_table.dim() != 2 or k.shape != v.shape:
         raise ValueError("page_table: [n_seq][width]; k and v alike")
     width = page_table.shape[1]
-    _on_device(cache.device, k=k, v=v, page_table=page_table, first=first, seq_start=seq_start)
+    dev = _device()
+    if (cache.index != dev or k.get_device() != dev or v.get_device() != dev or page_table.get_device() != dev
+            or first.get_device() != dev or seq_start.get_device() != dev):
+        _on_device(cache.device, k=k, v=v, page_table=page_table, first=first, seq_start=seq_start)
     kp, ks = _rows("k", k, cache.n_kv_heads, cache.head_dim, cache.dtype)
     vp, vs = _rows("v", v, cache.n_kv_heads, cache.head_dim, cache.dtype)
     rc = lib.s2moe_kv_write(cache._ref, int(layer), n_seq, k.shape[0], kp, ks, vp, vs, _int32("page_table", page_table, n_seq, width),
@@ -690,7 +711,10 @@ def kv_commit(cache: KVCache, page_table: torch.Tensor, context: torch.Tensor, p
     if page_table.dim() != 2 or path.dim() != 2:
         raise ValueError("page_table: [n_seq][width], path: [n_seq][most]")
     n_seq, width = page_table.shape
-    _on_device(cache.device, page_table=page_table, context=context, path=path, n_path=n_path)
+    dev = _device()
+    if (cache.index != dev or page_table.get_device() != dev or context.get_device() != dev or path.get_device() != dev
+            or n_path.get_device() != dev):
+        _on_device(cache.device, page_table=page_table, context=context, path=path, n_path=n_path)
     out = _output(out, context)
     rc = lib.s2moe_kv_commit(cache._ref, n_seq, _int32("page_table", page_table, n_seq, width), width,
                              _int32("context", context, n_seq), _int32("path", path, n_seq, path.shape[1]), path.shape[1],

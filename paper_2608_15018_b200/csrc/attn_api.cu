@@ -101,7 +101,7 @@ TreePlan tree_plan(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_hea
     if (dtype == S2MOE_F32) {
         p.rows_tile = rows <= 16 * (int64_t)n_seq ? 16 : 64;
         p.key_tile = kAttnSimpleTile;
-        p.min_units = 4;
+        p.min_units = 2;
         p.grid = 2 * n_sm;
     } else {
         p.pair = rows > (int64_t)n_seq * tc_rows(group);
@@ -198,8 +198,11 @@ int run_prompt(int dtype, AttnArgs a, cudaStream_t st)
 {
     const int64_t rows = (int64_t)a.n_tokens * a.group;
     if (dtype == S2MOE_F32) {
-        a.rows_tile = 64;
-        return launch_simple<D, 64, false, false>(a, grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq)), st);
+        // Few rows in all: with blocks of 64 the longest one alone would take the time of the call.  Measured, us, 16 / 64:
+        // 600 tokens of 8 heads of 64 41 / 60, 256 of 16 heads of 128 35 / 47, 600 103 / 109, beyond the line 1200 331 / 277
+        a.rows_tile = rows * a.Hk < 12288 ? 16 : 64;
+        const int64_t grid = grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq));
+        return a.rows_tile == 16 ? launch_simple<D, 16, false, false>(a, grid, st) : launch_simple<D, 64, false, false>(a, grid, st);
     }
     a.rows_tile = 2 * tc_rows(a.group);
     AttnMaps maps;
@@ -361,7 +364,7 @@ int s2moe_kv_write(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, in
     a.stride[0] = k_stride * es / 16; a.stride[1] = v_stride * es / 16;
     a.seq_start = seq_start; a.first = first; a.page_table = page_table;
     a.layer = layer; a.n_seq = n_seq; a.n_tokens = n_tokens; a.table_width = table_width;
-    kv_write_kernel<<<dim3((unsigned)((n_tokens + 3ll) / 4), 2), 128, 0, (cudaStream_t)cuda_stream>>>(a);
+    kv_write_kernel<<<(unsigned)((n_tokens + 3ll) / 4), 128, 0, (cudaStream_t)cuda_stream>>>(a);
     return launch_status();
 }
 
@@ -381,9 +384,18 @@ int s2moe_kv_commit(const s2moe_kv_cache *cache, int32_t n_seq, const int32_t *p
     a.pool[0] = (uint4 *)cache->k; a.pool[1] = (uint4 *)cache->v;
     a.page_table = page_table; a.context = context; a.path = path; a.n_path = n_path; a.new_context = new_context;
     a.n_seq = n_seq; a.table_width = table_width; a.max_path = max_path;
-    const int64_t per_seq = (int64_t)cache->n_layers * 2 * ((cache->n_kv_heads * a.c.row16 + 31) / 32);
+    const int64_t per_seq = (int64_t)cache->n_layers * ((cache->n_kv_heads * a.c.row16 + kKvCommitThreads - 1) / kKvCommitThreads);
     if (per_seq > 65535) return S2MOE_ERANGE;
-    kv_commit_kernel<<<dim3((unsigned)n_seq, (unsigned)per_seq), 32, 0, (cudaStream_t)cuda_stream>>>(a);
+    const dim3 grid((unsigned)n_seq, (unsigned)per_seq, 2);
+    const size_t smem = (size_t)max_path * kKvCommitThreads * 16;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (max_path <= kKvRegPath) kv_commit_kernel<true><<<grid, kKvCommitThreads, 0, st>>>(a);
+    else {
+        if (smem > 48 * 1024 && cudaFuncSetAttribute(kv_commit_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     kKvMaxPath * kKvCommitThreads * 16) != cudaSuccess)
+            return S2MOE_ECUDA;
+        kv_commit_kernel<false><<<grid, kKvCommitThreads, smem, st>>>(a);
+    }
     return launch_status();
 }
 

@@ -1,9 +1,14 @@
 // Attention on the CUDA cores, for binary32, and the kernel that joins the pieces of split items.
 //
-// A CTA of 256 threads holds R rows of q and takes the keys 64 at a time: scores by register tiles of R/16 rows x 4
-// keys per thread, the running maximum m and sum l of the softmax (p = 2^(s - m), l' = l 2^(m - m') + sum p, likewise
-// the product), then the product with the values by register tiles of R/16 rows x D/16 columns.  All of it in
-// binary32.
+// A CTA of 256 threads holds R rows of q and takes the keys 64 at a time: scores, the running maximum m and sum l of the
+// softmax (p = 2^(s - m), l' = l 2^(m - m') + sum p, likewise the product), then the product with the values.  All of it
+// in binary32.  What bounds it is reading the operands from shared memory (a 16-byte read takes a warp four cycles,
+// whatever the lanes have in common), so a thread computes a tile of its own of both products in registers:
+//   R = 64   4 rows x 4 keys, and 4 rows x D/16 columns
+//   R = 16   4 rows x 4 keys of a quarter of the D terms, and 4 rows x D/16 columns of a quarter of the keys, the quarters
+//            summed through shared memory (scores per tile, the product once per item); without the quarters a thread
+//            would have 1 x 4 scores and read more than twice as much.  The next tile is on its way in registers
+//            meanwhile.
 #pragma once
 
 #include "attn_common.cuh"
@@ -15,8 +20,9 @@ constexpr int kAttnSimpleTile = 64;       // keys of a tile
 
 __host__ __device__ constexpr int attn_simple_smem(int D, int R)
 {
-    // q rows, then the tile's keys (whose place the weights take once the scores are known), then its values
-    return 4 * (R * (D + 4) + (64 * (D + 4) > R * 68 ? 64 * (D + 4) : R * 68) + 64 * D);
+    // q rows, then the tile's keys (R = 64: whose place the weights take once the scores are known), then its values; R = 16:
+    // then the scores of the four quarters and the weights (the product's quarters take the place of the keys)
+    return 4 * (R * (D + 4) + 64 * (D + 4) + 64 * D + (R == 16 ? 4 * 16 * 66 + 16 * 68 + 16 : 0));
 }
 
 template <typename T>
@@ -64,7 +70,8 @@ __global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(Attn
 {
     constexpr int RT = R / 16, CT = D / 64, QP = D + 4, PP = 68;
     extern __shared__ __align__(16) float attn_smem[];
-    float *qs = attn_smem, *ks = qs + R * QP, *ps = ks, *vs = ks + (64 * QP > R * PP ? 64 * QP : R * PP);
+    float *qs = attn_smem, *ks = qs + R * QP, *vs = ks + 64 * QP, *parts = vs + 64 * D;     // (parts and behind: R = 16)
+    float *ps = R == 16 ? parts + 4 * 16 * 66 : ks, *fs = ps + 16 * PP;
     __shared__ int key_ok[64];
     const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
     if (SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // the joining kernel waits for the end
@@ -86,40 +93,171 @@ __global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(Attn
             }
             attn_store4(qs + r * QP + c, x);
         }
+        // (the tree's masks only for pieces that reach it)
+        const bool tree = PAGED && a.parent && !q.bad && p.t1 * kAttnSimpleTile > q.ctx;
+        unsigned long long nodes[2] = {0, 0};
+        if (tree) attn_ancestors_all(a, q, nodes);
         int lim[RT];
         unsigned long long anc[RT];
         float m[RT], l[RT], o[RT][4 * CT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
-            const int row = row0 + ty + 16 * i;
-            lim[i] = 0;
+            const int row = row0 + ty + 16 * i, token = row / a.group;
+            lim[i] = row < rows ? attn_limit<PAGED>(q, token) : 0;
             anc[i] = ~0ull;
-            if (row < rows) {
-                lim[i] = attn_limit<PAGED>(q, row / a.group);
-                if (PAGED && a.parent && !q.bad) anc[i] = attn_ancestors(a, q, q.nodes - q.n + row / a.group);
+            if (tree) {
+                const int node = min(max(q.nodes - q.n + token, 0), kAttnMaxNodes - 1);
+                const unsigned long long lo = __shfl_sync(0xffffffffu, nodes[0], node & 31), hi = __shfl_sync(0xffffffffu, nodes[1], node & 31);
+                anc[i] = node < 32 ? lo : hi;
             }
             m[i] = -CUDART_INF_F;
             l[i] = 0.f;
 #pragma unroll
             for (int c = 0; c < 4 * CT; ++c) o[i][c] = 0.f;
         }
-        for (int t = p.t0; t < p.t1; ++t) {
+        // a tile's keys and values: 4 threads per key
+        constexpr int LD = D / 16;
+        float4 kk_next[LD], vv_next[LD];             // (R = 16)
+        bool ok_next = false;
+        auto fetch = [&](int t, float4 *kk, float4 *vv) -> bool {
+            const int key = t * 64 + (tid >> 2);
+            long long ko = 0, vo = 0;
+            const bool ok = key < q.total && attn_key<PAGED, D>(a, q, p.s, p.h, key, ko, vo);
+#pragma unroll
+            for (int c = 0; c < LD; ++c) {
+                kk[c] = vv[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (ok) {
+                    kk[c] = attn_load4(reinterpret_cast<const T *>(a.k) + ko + (tid & 3) * 4 + 16 * c);
+                    vv[c] = attn_load4(reinterpret_cast<const T *>(a.v) + vo + (tid & 3) * 4 + 16 * c);
+                }
+            }
+            return ok;
+        };
+        auto place = [&](const float4 *kk, const float4 *vv, bool ok) {
+            const int r = tid >> 2;
+            if ((tid & 3) == 0) key_ok[r] = ok;
+#pragma unroll
+            for (int c = 0; c < LD; ++c) {
+                attn_store4(ks + r * QP + (tid & 3) * 4 + 16 * c, kk[c]);
+                attn_store4(vs + r * D + (tid & 3) * 4 + 16 * c, vv[c]);
+            }
+        };
+        if (R == 16) {
+            ok_next = fetch(p.t0, kk_next, vv_next);
+            float prod[4][D / 16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) prod[i][c] = 0.f;
+            const int quarter = tid >> 6, side = (tid >> 5) & 1, lx = lane & 7, r4 = (lane >> 3) * 4;
+            for (int t = p.t0; t < p.t1; ++t) {
+                __syncthreads();
+                place(kk_next, vv_next, ok_next);
+                __syncthreads();
+                if (t + 1 < p.t1) ok_next = fetch(t + 1, kk_next, vv_next);
+                {
+                    float acc[4][4];                     // rows r4 + i, keys 32 side + lx + 8 j, terms of the quarter
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+                    for (int c = quarter * (D / 4); c < (quarter + 1) * (D / 4); c += 4) {
+                        float4 kk[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) kk[j] = *reinterpret_cast<const float4 *>(ks + (32 * side + lx + 8 * j) * QP + c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 x = *reinterpret_cast<const float4 *>(qs + (r4 + i) * QP + c);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                acc[i][j] = fmaf(x.x, kk[j].x, fmaf(x.y, kk[j].y, fmaf(x.z, kk[j].z, fmaf(x.w, kk[j].w, acc[i][j]))));
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) parts[(quarter * 16 + r4 + i) * 66 + 32 * side + lx + 8 * j] = acc[i][j];
+                }
+                __syncthreads();
+                // 16 threads per row
+                float sc[4], mx = -CUDART_INF_F;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int key = tx + 16 * j;
+                    float x = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x += parts[(i * 16 + ty) * 66 + key];
+                    const bool sees = key_ok[key] != 0 && attn_sees(t * 64 + key, q.ctx, lim[0], anc[0]);
+                    sc[j] = sees ? x * a.scale_log2 : -CUDART_INF_F;
+                    mx = fmaxf(mx, sc[j]);
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+                const float mn = fmaxf(m[0], mx), off = mn == -CUDART_INF_F ? 0.f : mn, f = exp2f(m[0] - off);
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float w = exp2f(sc[j] - off);
+                    sum += w;
+                    ps[ty * PP + tx + 16 * j] = w;
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                l[0] = l[0] * f + sum;
+                m[0] = mn;
+                if (tx == 0) fs[ty] = f;
+                __syncthreads();
+                // rows r4 + i, columns D/2 side + 4 lx + 32 c, keys of the quarter
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c) prod[i][c] *= fs[r4 + i];
+#pragma unroll 2
+                for (int j = quarter * 16; j < quarter * 16 + 16; j += 4) {
+                    float4 w[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4 *>(ps + (r4 + i) * PP + j);
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) {
+                        float4 vv[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) vv[x] = *reinterpret_cast<const float4 *>(vs + (j + x) * D + D / 2 * side + 4 * lx + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float *oo = &prod[i][4 * c];
+                            oo[0] = fmaf(w[i].x, vv[0].x, fmaf(w[i].y, vv[1].x, fmaf(w[i].z, vv[2].x, fmaf(w[i].w, vv[3].x, oo[0]))));
+                            oo[1] = fmaf(w[i].x, vv[0].y, fmaf(w[i].y, vv[1].y, fmaf(w[i].z, vv[2].y, fmaf(w[i].w, vv[3].y, oo[1]))));
+                            oo[2] = fmaf(w[i].x, vv[0].z, fmaf(w[i].y, vv[1].z, fmaf(w[i].z, vv[2].z, fmaf(w[i].w, vv[3].z, oo[2]))));
+                            oo[3] = fmaf(w[i].x, vv[0].w, fmaf(w[i].y, vv[1].w, fmaf(w[i].z, vv[2].w, fmaf(w[i].w, vv[3].w, oo[3]))));
+                        }
+                    }
+                }
+            }
+            __syncthreads();                             // the quarters of the product, in the keys' place
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c)
+                    attn_store4(ks + (quarter * 16 + r4 + i) * QP + D / 2 * side + 4 * lx + 32 * c,
+                                make_float4(prod[i][4 * c], prod[i][4 * c + 1], prod[i][4 * c + 2], prod[i][4 * c + 3]));
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 x = *reinterpret_cast<const float4 *>(ks + (i * 16 + ty) * QP + 64 * c + 4 * tx);
+                    o[0][4 * c] += x.x;
+                    o[0][4 * c + 1] += x.y;
+                    o[0][4 * c + 2] += x.z;
+                    o[0][4 * c + 3] += x.w;
+                }
+        } else for (int t = p.t0; t < p.t1; ++t) {
             __syncthreads();
             {
-                const int r = tid >> 2, key = t * 64 + r;
-                long long ko = 0, vo = 0;
-                const bool ok = key < q.total && attn_key<PAGED, D>(a, q, p.s, p.h, key, ko, vo);
-                if ((tid & 3) == 0) key_ok[r] = ok;
-#pragma unroll 4
-                for (int c = (tid & 3) * 4; c < D; c += 16) {
-                    float4 kk = make_float4(0.f, 0.f, 0.f, 0.f), vv = kk;
-                    if (ok) {
-                        kk = attn_load4(reinterpret_cast<const T *>(a.k) + ko + c);
-                        vv = attn_load4(reinterpret_cast<const T *>(a.v) + vo + c);
-                    }
-                    attn_store4(ks + r * QP + c, kk);
-                    attn_store4(vs + r * D + c, vv);
-                }
+                float4 kk[LD], vv[LD];
+                const bool ok = fetch(t, kk, vv);
+                place(kk, vv, ok);
             }
             __syncthreads();
             float sc[RT][4];

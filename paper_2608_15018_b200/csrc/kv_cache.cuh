@@ -18,8 +18,8 @@ __device__ __forceinline__ long long kv_row(const KvShape &c, int layer, int pag
     return ((((long long)layer * c.n_pages + page) * c.heads + head) << c.page_shift) + at;
 }
 
-// One warp per token and matrix (blockIdx.y 0: keys, 1: values).  Tokens that belong to no sequence, positions outside the
-// table and pages outside the cache are left out.
+// One warp per token, keys and values.  Tokens that belong to no sequence, positions outside the table and pages outside the
+// cache are left out.
 struct KvWriteArgs {
     KvShape c;
     uint4 *dst[2];
@@ -30,7 +30,7 @@ struct KvWriteArgs {
 };
 __global__ void __launch_bounds__(128) kv_write_kernel(KvWriteArgs a)
 {
-    const int lane = threadIdx.x & 31, mat = blockIdx.y;
+    const int lane = threadIdx.x & 31;
     const int tok = blockIdx.x * 4 + (threadIdx.x >> 5);
     if (tok >= a.n_tokens) return;
     int pos = -1, s = -1;
@@ -53,26 +53,31 @@ __global__ void __launch_bounds__(128) kv_write_kernel(KvWriteArgs a)
     if (p < 0 || p >= ((long long)a.table_width << a.c.page_shift)) return;
     const int page = __ldg(a.page_table + (long long)s * a.table_width + (p >> a.c.page_shift));
     if ((unsigned)page >= (unsigned)a.c.n_pages) return;
-    const uint4 *src = a.src[mat] + (long long)tok * a.stride[mat];
-    uint4 *dst = a.dst[mat] + kv_row(a.c, a.layer, page, 0, (int)(p & ((1 << a.c.page_shift) - 1))) * a.c.row16;
+    const long long at = kv_row(a.c, a.layer, page, 0, (int)(p & ((1 << a.c.page_shift) - 1))) * a.c.row16;
     const int n = a.c.heads * a.c.row16;
     const long long head_step = (long long)a.c.row16 << a.c.page_shift;
-    for (int i0 = lane; i0 < n; i0 += 256) {
-        uint4 x[8];
+    for (int i0 = lane; i0 < n; i0 += 128) {
+        uint4 x[2][4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i0 + 32 * j < n) x[j] = __ldcs(src + i0 + 32 * j);
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < 4; ++j)
+                if (i0 + 32 * j < n) x[m][j] = __ldcs(a.src[m] + (long long)tok * a.stride[m] + i0 + 32 * j);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
             const int i = i0 + 32 * j;
-            if (i < n) dst[i / a.c.row16 * head_step + i % a.c.row16] = x[j];
+            if (i >= n) break;
+            const long long to = at + i / a.c.row16 * head_step + i % a.c.row16;
+            a.dst[0][to] = x[0][j];
+            a.dst[1][to] = x[1][j];
         }
     }
 }
 
-// One warp per sequence, layer, matrix and 32 words of a token's row of all heads: a thread reads its word of all accepted
-// rows before it writes any, so that paths in any order, and paths that name a node twice, move what stood there before the
-// call.  Up to 8 rows stay in registers (a path is rarely longer), more go through shared memory.
+// One block per sequence, layer, matrix and 128 words of a token's row of all heads: a thread reads its word of all
+// accepted rows before it writes any, so that paths in any order, and paths that name a node twice, move what stood there
+// before the call.  Paths of up to 16 stay in registers, longer ones go through shared memory (which would leave few
+// blocks on an SM: 48 paths over 32 layers took 35 us that way).
 struct KvCommitArgs {
     KvShape c;
     uint4 *pool[2];
@@ -80,19 +85,21 @@ struct KvCommitArgs {
     int32_t *new_context;
     int n_seq, table_width, max_path;
 };
-__global__ void __launch_bounds__(32) kv_commit_kernel(KvCommitArgs a)
+constexpr int kKvCommitThreads = 128, kKvRegPath = 16;
+template <bool REGS>
+__global__ void __launch_bounds__(kKvCommitThreads) kv_commit_kernel(KvCommitArgs a)
 {
-    __shared__ uint4 rows[kKvMaxPath][32];
-    __shared__ long long from[kKvMaxPath], to[kKvMaxPath];
-    const int lane = threadIdx.x, s = blockIdx.x;
-    const int chunks = (a.c.heads * a.c.row16 + 31) / 32;
-    const int chunk = blockIdx.y % chunks, mat = (blockIdx.y / chunks) & 1, layer = blockIdx.y / (2 * chunks);
+    extern __shared__ uint4 kv_rows[];           // !REGS: [row][thread]
+    __shared__ long long from[REGS ? kKvRegPath : kKvMaxPath], to[REGS ? kKvRegPath : kKvMaxPath];
+    const int tid = threadIdx.x, s = blockIdx.x;
+    const int chunks = (a.c.heads * a.c.row16 + kKvCommitThreads - 1) / kKvCommitThreads;
+    const int layer = blockIdx.y / chunks, chunk = blockIdx.y - layer * chunks;
     const int ctx = __ldg(a.context + s), n = min(max(__ldg(a.n_path + s), 0), a.max_path);
-    if (blockIdx.y == 0 && lane == 0) a.new_context[s] = ctx + n;
+    if (blockIdx.y == 0 && blockIdx.z == 0 && tid == 0) a.new_context[s] = ctx + n;
     const long long cap = (long long)a.table_width << a.c.page_shift;
     const int mask = (1 << a.c.page_shift) - 1;
     bool any = false;
-    for (int i = lane; i < n; i += 32) {
+    for (int i = tid; i < n; i += kKvCommitThreads) {
         const int node = __ldg(a.path + (long long)s * a.max_path + i);
         const long long src = (long long)ctx + node, dst = (long long)ctx + i;
         long long f = -1, t = -1;
@@ -100,34 +107,33 @@ __global__ void __launch_bounds__(32) kv_commit_kernel(KvCommitArgs a)
             const int32_t *table = a.page_table + (long long)s * a.table_width;
             const int ps = __ldg(table + (src >> a.c.page_shift)), pd = __ldg(table + (dst >> a.c.page_shift));
             if ((unsigned)ps < (unsigned)a.c.n_pages && (unsigned)pd < (unsigned)a.c.n_pages) {
-                f = kv_row(a.c, layer, ps, 0, (int)(src & mask));
-                t = kv_row(a.c, layer, pd, 0, (int)(dst & mask));
+                f = kv_row(a.c, layer, ps, 0, (int)(src & mask)) * a.c.row16;
+                t = kv_row(a.c, layer, pd, 0, (int)(dst & mask)) * a.c.row16;
                 any = true;
             }
         }
         from[i] = f;
         to[i] = t;
     }
-    if (!__any_sync(0xffffffffu, any)) return;
-    __syncwarp();
-    const int i = chunk * 32 + lane;
+    if (!__syncthreads_or(any)) return;
+    const int i = chunk * kKvCommitThreads + tid;
     if (i >= a.c.heads * a.c.row16) return;
     const long long off = (long long)(i / a.c.row16) * ((long long)a.c.row16 << a.c.page_shift) + i % a.c.row16;
-    uint4 *pool = a.pool[mat] + off;
-    if (n <= 8) {
-        uint4 x[8];
+    uint4 *pool = a.pool[blockIdx.z] + off;
+    if (REGS) {
+        uint4 x[kKvRegPath];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n && from[j] >= 0) x[j] = pool[from[j] * a.c.row16];
+        for (int j = 0; j < kKvRegPath; ++j)
+            if (j < n && from[j] >= 0) x[j] = pool[from[j]];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n && from[j] >= 0) pool[to[j] * a.c.row16] = x[j];
+        for (int j = 0; j < kKvRegPath; ++j)
+            if (j < n && from[j] >= 0) pool[to[j]] = x[j];
     } else {
 #pragma unroll 8
         for (int j = 0; j < n; ++j)
-            if (from[j] >= 0) rows[j][lane] = pool[from[j] * a.c.row16];
+            if (from[j] >= 0) kv_rows[j * kKvCommitThreads + tid] = pool[from[j]];
         for (int j = 0; j < n; ++j)
-            if (from[j] >= 0) pool[to[j] * a.c.row16] = rows[j][lane];
+            if (from[j] >= 0) pool[to[j]] = kv_rows[j * kKvCommitThreads + tid];
     }
 }
 

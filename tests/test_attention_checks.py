@@ -95,7 +95,7 @@ def test_kv_commit_refuses():
               dict(n_path=None), dict(new_context=None), dict(new_context=P), dict(new_context=P + 4)):
         assert call(**f) == binding.EINVAL, f
     assert call(max_path=65) == binding.ERANGE
-    assert call(cache(n_layers=32768)) == binding.ERANGE
+    assert call(cache(n_layers=65536)) == binding.ERANGE
     assert call(n_seq=0) == binding.OK
 
 
@@ -128,6 +128,8 @@ def library(monkeypatch):
     lib = _Library()
     monkeypatch.setattr(binding, "load_library", lambda: lib)
     monkeypatch.setattr(binding, "_on_device", lambda device, **tensors: None)
+    monkeypatch.setattr(binding, "_device", lambda: 0)
+    monkeypatch.setattr(binding, "_tree_workspace", lambda *sizes: 0)
     monkeypatch.setattr(binding, "_dptr", lambda t: t.data_ptr())
     monkeypatch.setattr(binding, "_stream_handle", lambda stream: 0)
     return lib
