@@ -213,18 +213,26 @@ int run_prompt(int dtype, AttnArgs a, cudaStream_t st)
     return launch_tc<D, false, true, false>(maps, a, grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq)), st);
 }
 
+template <typename T, int D, int KEY_TILE>
+int launch_join(const AttnArgs &a, const TreePlan &p, cudaStream_t st)
+{
+    const int64_t rows = (int64_t)a.n_tokens * a.Hk * a.group;
+    return p.items * 8 <= p.grid ? launch<attn_join_kernel<T, D, KEY_TILE, 4>>(rows, 128, 0, st, true, a, p.grid)
+                                 : launch<attn_join_kernel<T, D, KEY_TILE, 1>>((rows + 3) / 4, 128, 0, st, true, a, p.grid);
+}
+
 template <int D>
 int run_tree(int dtype, AttnArgs a, const TreePlan &p, cudaStream_t st)
 {
     a.rows_tile = p.rows_tile;
     a.min_units = p.min_units;
-    const int64_t grid = p.split ? p.grid : grid_for(p.items), join = ((int64_t)a.n_tokens * a.Hk * a.group + 3) / 4;
+    const int64_t grid = p.split ? p.grid : grid_for(p.items);
     int rc;
     if (dtype == S2MOE_F32) {
         if (p.rows_tile == 16) rc = p.split ? launch_simple<D, 16, true, true>(a, grid, st) : launch_simple<D, 16, true, false>(a, grid, st);
         else rc = p.split ? launch_simple<D, 64, true, true>(a, grid, st) : launch_simple<D, 64, true, false>(a, grid, st);
         if (rc != S2MOE_OK || !p.split) return rc;
-        return launch<attn_join_kernel<float, D, kAttnSimpleTile>>(join, 128, 0, st, true, a, p.grid);
+        return launch_join<float, D, kAttnSimpleTile>(a, p, st);
     }
     const int page = 1 << a.page_shift;
     const int64_t rows = (int64_t)a.n_pages * a.Hk;
@@ -236,7 +244,7 @@ int run_tree(int dtype, AttnArgs a, const TreePlan &p, cudaStream_t st)
     if (p.pair) rc = p.split ? launch_tc<D, true, true, true>(maps, a, grid, st) : launch_tc<D, true, true, false>(maps, a, grid, st);
     else rc = p.split ? launch_tc<D, true, false, true>(maps, a, grid, st) : launch_tc<D, true, false, false>(maps, a, grid, st);
     if (rc != S2MOE_OK || !p.split) return rc;
-    return launch<attn_join_kernel<__nv_bfloat16, D, kAttnTile>>(join, 128, 0, st, true, a, p.grid);
+    return launch_join<__nv_bfloat16, D, kAttnTile>(a, p, st);
 }
 
 }  // namespace

@@ -37,8 +37,8 @@ template <int D, bool PAIR>
 struct AttnSmem {
     static constexpr int tile = kAttnHalf * (D / 64);
     static constexpr int q = tile * (PAIR ? 2 : 1);
-    static constexpr int slots = D == 128 ? 5 : 8;
-    static constexpr int bytes = q + slots * tile + 1024;       // + alignment to the swizzle's 1024 bytes
+    static constexpr int slots = D == 128 ? (PAIR ? 5 : 6) : 8;
+    static constexpr int bytes = q + slots * tile;              // D = 128: with up to 3 KB of static memory all that a CTA can have
 };
 
 struct AttnMaps {
@@ -121,13 +121,17 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     using L = AttnSmem<D, PAIR>;
     using Iter = AttnIter<PAGED, SPLIT, kAttnTile>;
     constexpr int NS = L::slots;
-    extern __shared__ uint8_t attn_raw[];
+    extern __shared__ __align__(1024) uint8_t attn_raw[];         // (the swizzle's period)
     __shared__ __align__(8) uint64_t full[NS], empty[NS], q_full[2], q_empty[2], s_full[2], o_full[2], p_part[2], p_full[2], ended[2], turn_of[2], n_full[2], n_empty[2], taken;
     __shared__ __align__(16) uint4 next_cta;
     __shared__ AttnPiece piece[2];                                // what the copying warp has found, one piece ahead
     __shared__ uint32_t tmem_at;
     __shared__ float2 ml[2][128];
-    uint8_t *qs = attn_raw + ((1024u - (smem_u32(attn_raw) & 1023u)) & 1023u), *ring = qs + L::q;
+    uint8_t *qs = attn_raw, *ring = qs + L::q;
+    if (smem_u32(attn_raw) & 1023u) {                             // (never seen; the tiles would be scrambled)
+        if (threadIdx.x == 0) atomicExch(a.status, ST_BAD_PLAN);
+        return;
+    }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int half = PAIR ? a.rows_tile / 2 : a.rows_tile;        // rows of a block that are in use
     if (SPLIT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -178,10 +182,25 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         const int last = min(p.q.n, first_tok + tok_half) - 1;
         return min(nt, (attn_limit<PAGED>(p.q, last) + kAttnTile - 1) / kAttnTile);
     };
-    // A softmax thread holds a row of S (128 registers).  The launch gives 384 threads 168 registers each; moved about, 128
-    // threads keep 72 and 256 have 216, which is the same sum.
     AttnPiece p;
     unsigned r0 = 0, pieces = 0;                                  // tiles and pieces before this one
+    unsigned r1 = 0;                                              // !PAIR: r0 counts the tiles of group 0, r1 those of group 1
+    // Place of a tile's keys (kv = 0) or values (1).  PAIR: one ring, both groups go through all of it.  !PAIR: a ring for
+    // each group: a barrier says whether a phase is odd or even, so whoever waits must have seen the phase before it, and
+    // of the other group's tiles a group knows nothing.
+    auto spot = [&](int t, int kv, unsigned &parity) -> unsigned {
+        constexpr unsigned N = PAIR ? NS : NS / 2;
+        const unsigned n = PAIR ? 2 * (r0 + t) + kv : 2 * ((t & 1 ? r1 : r0) + t / 2) + kv, turn = n / N;
+        parity = turn & 1u;
+        return n - turn * N + (!PAIR && (t & 1) ? N : 0u);
+    };
+    auto passed = [&](int nt) {                                   // a piece is done with
+        r0 += PAIR ? nt : (nt + 1) / 2;
+        if (!PAIR) r1 += nt / 2;
+        ++pieces;
+    };
+    // A softmax thread holds a row of S (128 registers).  The launch gives 384 threads 168 registers each; moved about, 128
+    // threads keep 72 and 256 have 216, which is the same sum.
     // The copying warp looks for the pieces and is ahead of the others by what the ring holds; they read what it found.
     auto next = [&]() -> bool {
         const unsigned b = pieces & 1u;
@@ -241,35 +260,41 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 mbar_arrive(&n_full[b]);
             }
             if (!more || !__all_sync(0xffffffffu, ok)) break;
-            for (int t = p.t0; t < p.t1 && __all_sync(0xffffffffu, ok); ++t) {
+            const int nt = p.t1 - p.t0;
+            auto fetch = [&](int t, int kv) {
                 int x = 0;                                        // this lane's page, as the tensor's last coordinate
                 if (PAGED && lane < ppt) {
-                    const int at = t * ppt + lane;
+                    const int at = (p.t0 + t) * ppt + lane;
                     x = a.n_pages * a.Hk;
                     if (at << a.page_shift < p.q.total) {
                         const int page = __ldg(a.page_table + (long long)p.s * a.table_width + at);
                         if ((unsigned)page < (unsigned)a.n_pages) x = page * a.Hk + p.h;
                     }
                 }
-                for (int kv = 0; kv < 2; ++kv) {
-                    const unsigned n = 2 * (r0 + (t - p.t0)) + kv, slot = n % NS;
-                    wait(&empty[slot], ((n / NS) & 1u) ^ 1u);
-                    if (lane == 0) mbar_expect_tx(&full[slot], L::tile);
-                    __syncwarp();
-                    uint8_t *dst = ring + slot * L::tile;
-                    const CUtensorMap *map = kv ? &maps.v : &maps.k;
-                    if (PAGED) {
-                        if (lane < ppt)
-                            for (int c = 0; c < D / 64; ++c)
-                                tma_load_3d(dst + c * kAttnHalf + ((lane * 128) << a.page_shift), map, 64 * c, 0, x, &full[slot]);
-                    } else if (lane < D / 64) {
-                        tma_load_3d(dst + lane * kAttnHalf, map, 64 * lane, p.h, p.q.tok0 + t * kAttnTile, &full[slot]);
-                    }
-                    __syncwarp();
+                unsigned parity;
+                const unsigned slot = spot(t, kv, parity);
+                wait(&empty[slot], parity ^ 1u);
+                if (lane == 0) mbar_expect_tx(&full[slot], L::tile);
+                __syncwarp();
+                uint8_t *dst = ring + slot * L::tile;
+                const CUtensorMap *map = kv ? &maps.v : &maps.k;
+                if (PAGED) {
+                    if (lane < ppt)
+                        for (int c = 0; c < D / 64; ++c)
+                            tma_load_3d(dst + c * kAttnHalf + ((lane * 128) << a.page_shift), map, 64 * c, 0, x, &full[slot]);
+                } else if (lane < D / 64) {
+                    tma_load_3d(dst + lane * kAttnHalf, map, 64 * lane, p.h, p.q.tok0 + (p.t0 + t) * kAttnTile, &full[slot]);
                 }
+                __syncwarp();
+            };
+            // in the order in which they are needed: K0 V0 K1 V1 ..., or, with two scores under way, K0 K1 V0 K2 V1 K3 ...
+            constexpr int kAhead = PAIR ? 0 : 2;
+            for (int i = -kAhead; i < nt && __all_sync(0xffffffffu, ok); ++i) {
+                if (PAIR) fetch(i, 0);
+                if (i >= 0) fetch(i, 1);
+                if (!PAIR && i + kAhead < nt) fetch(i + kAhead, 0);
             }
-            r0 += p.t1 - p.t0;
-            ++pieces;
+            passed(p.t1 - p.t0);
         }
         // nothing may land in shared memory that is no longer this CTA's
         if (!ok) {
@@ -312,8 +337,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             if (leader && ok) {
                 const int n = tiles_of(p, w), nt = p.t1 - p.t0;
                 auto arrived = [&](int t, int kv) -> unsigned {   // slot of a tile of the piece, once it is there
-                    const unsigned c = 2 * (r0 + t) + kv, slot = c % NS;
-                    wait(&full[slot], (c / NS) & 1u);
+                    unsigned parity;
+                    const unsigned slot = spot(t, kv, parity);
+                    wait(&full[slot], parity);
                     return slot;
                 };
                 auto scores = [&](int t) {                        // S = Q K^T, then K's slot is free
@@ -384,8 +410,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                         for (int kv = 0; kv < 2; ++kv) mbar_arrive(&empty[arrived(t, kv)]);
             }
             __syncwarp();
-            r0 += p.t1 - p.t0;
-            ++pieces;
+            passed(p.t1 - p.t0);
         }
         if (leader && !ok) {                                      // no instruction outlives the CTA's tensor memory
             tc_commit(&ended[w]);
@@ -426,19 +451,23 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 }
                 if (!have_anc && key0 + kAttnTile > q.ctx) {        // the first tile with nodes of the tree
                     have_anc = true;
-                    unsigned long long all_nodes[2];
-                    attn_ancestors_all(a, q, all_nodes);
-                    const int node = min(max(q.nodes - q.n + token, 0), kAttnMaxNodes - 1);
-                    const unsigned long long lo = __shfl_sync(0xffffffffu, all_nodes[0], node & 31), hi = __shfl_sync(0xffffffffu, all_nodes[1], node & 31);
-                    anc = node < 32 ? lo : hi;
+                    anc = 1;
+                    if (q.nodes > 1) {
+                        unsigned long long all_nodes[2];
+                        attn_ancestors_all(a, q, all_nodes);
+                        const int node = min(max(q.nodes - q.n + token, 0), kAttnMaxNodes - 1);
+                        const unsigned long long lo = __shfl_sync(0xffffffffu, all_nodes[0], node & 31), hi = __shfl_sync(0xffffffffu, all_nodes[1], node & 31);
+                        anc = node < 32 ? lo : hi;
+                    }
                 }
                 wait(&s_full[w], s_phase);
                 s_phase ^= 1u;
                 tc_fence_after();
                 if (key0 + kAttnTile > q.total) {
                     // rows of V behind the last key can hold anything, and 0 * NaN is no 0
-                    const unsigned c = 2 * (r0 + t) + 1, slot = c % NS;
-                    wait(&full[slot], (c / NS) & 1u);
+                    unsigned parity;
+                    const unsigned slot = spot(t, 1, parity);
+                    wait(&full[slot], parity);
                     if (key0 + row_in >= q.total) {
                         uint4 *v = reinterpret_cast<uint4 *>(ring + slot * L::tile + row_in * 128);
 #pragma unroll
@@ -587,8 +616,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                 }
                 hand_over(&p_full[w]);
             }
-            r0 += p.t1 - p.t0;
-            ++pieces;
+            passed(p.t1 - p.t0);
             if (n > 0) {
                 wait(&o_full[w], o_phase);
                 o_phase ^= 1u;
