@@ -552,9 +552,18 @@ def _rows(name: str, t: torch.Tensor, heads: int, dim: int, dtype: torch.dtype) 
     return address, stride
 
 
-def _output(out: Optional[torch.Tensor], like: torch.Tensor) -> torch.Tensor:
+def _new(like: torch.Tensor, stream: Optional[torch.cuda.Stream], nbytes: int = 0) -> torch.Tensor:
+    """Memory like ``like`` (or ``nbytes`` bytes) that belongs to the stream of the call: what the allocator hands out on
+    another stream may still be read there."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _new(like, None, nbytes)
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
+def _output(out: Optional[torch.Tensor], like: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     if out is None:
-        return torch.empty_like(like, memory_format=torch.contiguous_format)
+        return _new(like, stream)
     if out.dtype != like.dtype or out.shape != like.shape or not out.is_contiguous() or out.device != like.device:
         raise ValueError(f"out: contiguous {like.dtype} {list(like.shape)} on {like.device} expected")
     return out
@@ -605,7 +614,7 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seq_star
     kp, ks = _rows("k", k, k.shape[1], dim, q.dtype)
     vp, vs = _rows("v", v, k.shape[1], dim, q.dtype)
     starts = _int32("seq_start", seq_start, n_seq + 1)
-    out = _output(out, q)
+    out = _output(out, q, stream)
     rc = lib.s2moe_prompt_attention(_DTYPES[q.dtype], n_seq, n, heads, k.shape[1], dim, qp, qs, kp, ks, vp, vs, starts,
                                     dim ** -0.5 if scale is None else float(scale), out.data_ptr(), _stream_handle(stream))
     if rc != OK:
@@ -654,15 +663,9 @@ def tree_attention(q: torch.Tensor, cache: KVCache, layer: int, page_table: torc
     table, ctx = _int32("page_table", page_table, n_seq, width), _int32("context", context, n_seq)
     starts, nodes = _int32("seq_start", seq_start, n_seq + 1), _int32("node_start", node_start, n_seq + 1)
     par = _int32("parent", parent, n_nodes)
-    out = _output(out, q)
+    out = _output(out, q, stream)
     need = _tree_workspace(dev, _DTYPES[cache.dtype], cache.n_kv_heads, cache.page_size, dim, n_seq, n, heads, width)
-    ws = None
-    if need:
-        if stream is None:
-            ws = q.new_empty(need, dtype=torch.uint8)
-        else:
-            with torch.cuda.stream(stream):
-                ws = q.new_empty(need, dtype=torch.uint8)
+    ws = _new(q, stream, need) if need else None
     rc = lib.s2moe_tree_attention(cache._ref, int(layer), n_seq, n, heads, qp, qs, table, width, ctx, starts, n_nodes, nodes, par,
                                   dim ** -0.5 if scale is None else float(scale), out.data_ptr(),
                                   None if ws is None else ws.data_ptr(), need, _stream_handle(stream))
@@ -715,7 +718,7 @@ def kv_commit(cache: KVCache, page_table: torch.Tensor, context: torch.Tensor, p
     if (cache.index != dev or page_table.get_device() != dev or context.get_device() != dev or path.get_device() != dev
             or n_path.get_device() != dev):
         _on_device(cache.device, page_table=page_table, context=context, path=path, n_path=n_path)
-    out = _output(out, context)
+    out = _output(out, context, stream)
     rc = lib.s2moe_kv_commit(cache._ref, n_seq, _int32("page_table", page_table, n_seq, width), width,
                              _int32("context", context, n_seq), _int32("path", path, n_seq, path.shape[1]), path.shape[1],
                              _int32("n_path", n_path, n_seq), out.data_ptr(), _stream_handle(stream))

@@ -83,7 +83,7 @@ int launch_status() { return cudaGetLastError() == cudaSuccess ? S2MOE_OK : S2MO
 // The launch plan of a tree attention call: a function of what the host knows, the same in the call and in the
 // workspace query.
 struct TreePlan {
-    int rows_tile, grid, min_units, key_tile;
+    int rows_tile, grid, min_units, key_tile, n_sm;
     bool split, pair;
     bool countable;                // the kernels count the units of a call in 32 bits
     int64_t items;                 // upper bound
@@ -96,6 +96,7 @@ int tc_rows(int group) { return kAttnTile / group * group; }
 TreePlan tree_plan(int dtype, int n_seq, int n_tokens, int n_heads, int n_kv_heads, int64_t capacity, int head_dim, int n_sm)
 {
     TreePlan p{};
+    p.n_sm = n_sm;
     const int group = n_heads / n_kv_heads;
     const int64_t rows = (int64_t)n_tokens * group;
     if (dtype == S2MOE_F32) {
@@ -179,8 +180,6 @@ int launch(int64_t grid, int threads, size_t smem, cudaStream_t st, bool behind,
 // at 1e-30 every weight is 1 as well.
 float scale_log2(float scale) { return scale < 1e-30f ? 1e-30f : scale * 1.44269504f; }
 
-int64_t grid_for(int64_t items) { return items < (1 << 20) ? items : 1 << 20; }
-
 template <int D, int R, bool PAGED, bool SPLIT>
 int launch_simple(const AttnArgs &a, int64_t grid, cudaStream_t st)
 {
@@ -193,15 +192,19 @@ int launch_tc(const AttnMaps &maps, const AttnArgs &a, int64_t grid, cudaStream_
     return launch<attn_tc_kernel<D, PAGED, PAIR, SPLIT>>(grid, kAttnThreads, (size_t)AttnSmem<D, PAIR>::bytes, st, false, maps, a);
 }
 
+// Blocks of the CUDA-core kernel without a split take every gridDim.x-th item; each looks for its first one from the
+// first sequence on, so that there must not be one per item where there are very many sequences.
+int64_t simple_grid(int64_t items, int n_sm) { return items < 16 * n_sm ? items : 16 * n_sm; }
+
 template <int D>
-int run_prompt(int dtype, AttnArgs a, cudaStream_t st)
+int run_prompt(int dtype, AttnArgs a, int n_sm, cudaStream_t st)
 {
     const int64_t rows = (int64_t)a.n_tokens * a.group;
     if (dtype == S2MOE_F32) {
         // Few rows in all: with blocks of 64 the longest one alone would take the time of the call.  Measured, us, 16 / 64:
         // 600 tokens of 8 heads of 64 41 / 60, 256 of 16 heads of 128 35 / 47, 600 103 / 109, beyond the line 1200 331 / 277
         a.rows_tile = rows * a.Hk < 12288 ? 16 : 64;
-        const int64_t grid = grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq));
+        const int64_t grid = simple_grid((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq), n_sm);
         return a.rows_tile == 16 ? launch_simple<D, 16, false, false>(a, grid, st) : launch_simple<D, 64, false, false>(a, grid, st);
     }
     a.rows_tile = 2 * tc_rows(a.group);
@@ -210,15 +213,20 @@ int run_prompt(int dtype, AttnArgs a, cudaStream_t st)
         !make_map(&maps.k, a.k, D, a.Hk, a.n_tokens, D, a.k_stride, 1, kAttnTile) ||
         !make_map(&maps.v, a.v, D, a.Hk, a.n_tokens, D, a.v_stride, 1, kAttnTile))
         return S2MOE_ECUDA;
-    return launch_tc<D, false, true, false>(maps, a, grid_for((int64_t)a.Hk * (rows / a.rows_tile + a.n_seq)), st);
+    // (a block per item: the blocks are the items' numbers)
+    return launch_tc<D, false, true, false>(maps, a, (int64_t)a.Hk * (rows / a.rows_tile + a.n_seq), st);
 }
 
 template <typename T, int D, int KEY_TILE>
 int launch_join(const AttnArgs &a, const TreePlan &p, cudaStream_t st)
 {
-    const int64_t rows = (int64_t)a.n_tokens * a.Hk * a.group;
-    return p.items * 8 <= p.grid ? launch<attn_join_kernel<T, D, KEY_TILE, 4>>(rows, 128, 0, st, true, a, p.grid)
-                                 : launch<attn_join_kernel<T, D, KEY_TILE, 1>>((rows + 3) / 4, 128, 0, st, true, a, p.grid);
+    const int Hq = a.Hk * a.group;
+    const int64_t rows = (int64_t)a.n_tokens * Hq;
+    if (p.items * 8 <= p.grid) return launch<attn_join_kernel<T, D, KEY_TILE, 4>>(rows, 128, 0, st, true, a, p.grid, 1);
+    // where there are rows enough for all SMs a warp takes several of one token: it looks for its sequence once
+    int each = 1;
+    while (each < 8 && Hq % (2 * each) == 0 && rows / (2 * each) >= 32ll * p.n_sm) each *= 2;
+    return launch<attn_join_kernel<T, D, KEY_TILE, 1>>((rows / each + 3) / 4, 128, 0, st, true, a, p.grid, each);
 }
 
 template <int D>
@@ -226,7 +234,7 @@ int run_tree(int dtype, AttnArgs a, const TreePlan &p, cudaStream_t st)
 {
     a.rows_tile = p.rows_tile;
     a.min_units = p.min_units;
-    const int64_t grid = p.split ? p.grid : grid_for(p.items);
+    const int64_t grid = p.split ? p.grid : dtype == S2MOE_F32 ? simple_grid(p.items, p.n_sm) : p.items;
     int rc;
     if (dtype == S2MOE_F32) {
         if (p.rows_tile == 16) rc = p.split ? launch_simple<D, 16, true, true>(a, grid, st) : launch_simple<D, 16, true, false>(a, grid, st);
@@ -277,7 +285,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     if (!facts) return S2MOE_ECUDA;
     a.status = facts->status;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    return head_dim == 64 ? run_prompt<64>(dtype, a, st) : run_prompt<128>(dtype, a, st);
+    return head_dim == 64 ? run_prompt<64>(dtype, a, facts->n_sm, st) : run_prompt<128>(dtype, a, facts->n_sm, st);
 }
 
 int s2moe_tree_attention_workspace(const s2moe_kv_cache *cache, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t table_width,

@@ -374,14 +374,14 @@ __global__ void __launch_bounds__(kAttnSimpleThreads, 2) attn_simple_kernel(Attn
 //   M = max m_i, out = sum_i o_i 2^(m_i - M) / sum_i l_i 2^(m_i - M)
 // The kernel in front may still run: what depends on the lengths alone is worked out before the wait for its end.
 template <typename T, int D, int KEY_TILE, int WARPS>
-__global__ void __launch_bounds__(128) attn_join_kernel(AttnArgs a, int grid)
+__global__ void __launch_bounds__(128) attn_join_kernel(AttnArgs a, int grid, int each)
 {
     constexpr int C = D / 32;
     __shared__ float part[WARPS][D];
     __shared__ float2 part_ml[WARPS];
     const int lane = threadIdx.x & 31, warp = WARPS > 1 ? threadIdx.x >> 5 : 0, Hq = a.Hk * a.group;
-    const long long row_id = WARPS > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int tok = (int)(row_id / Hq), head = (int)(row_id - (long long)tok * Hq), h = head / a.group;
+    const long long row_id = WARPS > 1 ? (long long)blockIdx.x : ((long long)blockIdx.x * 4 + (threadIdx.x >> 5)) * each;
+    const int tok = (int)(row_id / Hq), head0 = (int)(row_id - (long long)tok * Hq);
     AttnIter<true, true, KEY_TILE> it(a, lane);
     it.load(0);
     const AttnCut cut(a, it.all_units(), grid);
@@ -394,80 +394,83 @@ __global__ void __launch_bounds__(128) attn_join_kernel(AttnArgs a, int grid)
         it.load(it.chunk + 32);
     }
     AttnPiece p;
-    int c0 = 0, c1 = 0, t = 0, r = 0, u0 = 0;
+    int t = 0, tiles = 1, blocks = 0, first = 0;
     if (hit) {
         const int l0 = __ffs((int)hit) - 1;
         it.take(l0, p);
         t = tok - p.q.tok0;
-        const int tiles = it.tiles(p.q), row = t * a.group + head - h * a.group, rt = row / a.rows_tile;
-        r = row - rt * a.rows_tile;
-        u0 = it.base + __shfl_sync(0xffffffffu, it.inc - it.my, l0) + (h * __shfl_sync(0xffffffffu, it.rts, l0) + rt) * tiles;
-        c0 = cut.owner(u0);
-        c1 = cut.owner(u0 + tiles - 1);
+        tiles = it.tiles(p.q);
+        blocks = __shfl_sync(0xffffffffu, it.rts, l0);
+        first = it.base + __shfl_sync(0xffffffffu, it.inc - it.my, l0);
     }
     // (every thread waits: what follows in the stream starts when this kernel has ended, and the one in front must have too)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (!hit || c0 == c1) return;                              // a whole item is written out already
-    const bool second = cut.start(c0) < u0;                    // the first piece is its CTA's second
-    float m = -CUDART_INF_F, l = 0.f, o[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) o[i] = 0.f;
-#pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += WARPS) {
-        const long long at = (2ll * c + (c == c0 && second ? 1 : 0)) * a.rows_tile + r;
-        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
-        float x[C];
-        if (C == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * lane);
-        else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(a.part_o + at * D + 2 * lane);
-        const float mn = fmaxf(m, ml.x), b = mn == -CUDART_INF_F ? 0.f : mn;
-        const float f = exp2f(m - b), e = exp2f(ml.x - b);
-        m = mn;
-        l = l * f + ml.y * e;
-#pragma unroll
-        for (int i = 0; i < C; ++i) o[i] = o[i] * f + x[i] * e;
-    }
-    if (WARPS > 1) {
-#pragma unroll
-        for (int i = 0; i < C; ++i) part[warp][C * lane + i] = o[i];
-        if (lane == 0) part_ml[warp] = make_float2(m, l);
-        __syncthreads();
-        if (warp > 0) return;
-        m = -CUDART_INF_F;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, part_ml[w].x);
-        const float b = m == -CUDART_INF_F ? 0.f : m;
-        l = 0.f;
+    if (!hit) return;
+    for (int head = head0; head < head0 + each; ++head) {
+        const int h = head / a.group, row = t * a.group + head - h * a.group, rt = row / a.rows_tile, r = row - rt * a.rows_tile;
+        const int u0 = first + (h * blocks + rt) * tiles, c0 = cut.owner(u0), c1 = cut.owner(u0 + tiles - 1);
+        if (c0 == c1) continue;                                    // a whole item is written out already
+        const bool second = cut.start(c0) < u0;                    // the first piece is its CTA's second
+        float m = -CUDART_INF_F, l = 0.f, o[C];
 #pragma unroll
         for (int i = 0; i < C; ++i) o[i] = 0.f;
+#pragma unroll 4
+        for (int c = c0 + warp; c <= c1; c += WARPS) {
+            const long long at = (2ll * c + (c == c0 && second ? 1 : 0)) * a.rows_tile + r;
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * at);
+            float x[C];
+            if (C == 4) *reinterpret_cast<float4 *>(x) = *reinterpret_cast<const float4 *>(a.part_o + at * D + 4 * lane);
+            else *reinterpret_cast<float2 *>(x) = *reinterpret_cast<const float2 *>(a.part_o + at * D + 2 * lane);
+            const float mn = fmaxf(m, ml.x), b = mn == -CUDART_INF_F ? 0.f : mn;
+            const float f = exp2f(m - b), e = exp2f(ml.x - b);
+            m = mn;
+            l = l * f + ml.y * e;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float e = exp2f(part_ml[w].x - b);
-            l += part_ml[w].y * e;
-#pragma unroll
-            for (int i = 0; i < C; ++i) o[i] += part[w][C * lane + i] * e;
+            for (int i = 0; i < C; ++i) o[i] = o[i] * f + x[i] * e;
         }
-    }
-    const float inv = p.q.bad ? CUDART_NAN_F : 1.f / l;
-    bool fine = true;
+        if (WARPS > 1) {                                           // (each = 1)
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        o[i] *= inv;
-        fine = fine && attn_finite(o[i]);
-    }
-    T *dst = reinterpret_cast<T *>(a.out) + ((long long)tok * Hq + head) * D;
-    if (!p.q.bad && __any_sync(0xffffffffu, !fine)) {
-        float x[C];
-        if (attn_row_again<T, D, true>(a, p.q, p.s, h, t, head, p.q.total, l == 0.f, x)) {
+            for (int i = 0; i < C; ++i) part[warp][C * lane + i] = o[i];
+            if (lane == 0) part_ml[warp] = make_float2(m, l);
+            __syncthreads();
+            if (warp > 0) return;
+            m = -CUDART_INF_F;
 #pragma unroll
-            for (int i = 0; i < C; ++i) dst[lane + 32 * i] = (T)x[i];
-            return;
+            for (int w = 0; w < WARPS; ++w) m = fmaxf(m, part_ml[w].x);
+            const float b = m == -CUDART_INF_F ? 0.f : m;
+            l = 0.f;
+#pragma unroll
+            for (int i = 0; i < C; ++i) o[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float e = exp2f(part_ml[w].x - b);
+                l += part_ml[w].y * e;
+#pragma unroll
+                for (int i = 0; i < C; ++i) o[i] += part[w][C * lane + i] * e;
+            }
         }
-    }
-    if (C == 4) {
-        attn_store4(dst + 4 * lane, make_float4(o[0], o[1], o[C - 2], o[C - 1]));
-    } else {
-        dst[2 * lane] = (T)o[0];
-        dst[2 * lane + 1] = (T)o[1];
+        const float inv = p.q.bad ? CUDART_NAN_F : 1.f / l;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            o[i] *= inv;
+            fine = fine && attn_finite(o[i]);
+        }
+        T *dst = reinterpret_cast<T *>(a.out) + ((long long)tok * Hq + head) * D;
+        if (!p.q.bad && __any_sync(0xffffffffu, !fine)) {
+            float x[C];
+            if (attn_row_again<T, D, true>(a, p.q, p.s, h, t, head, p.q.total, l == 0.f, x)) {
+#pragma unroll
+                for (int i = 0; i < C; ++i) dst[lane + 32 * i] = (T)x[i];
+                continue;
+            }
+        }
+        if (C == 4) {
+            attn_store4(dst + 4 * lane, make_float4(o[0], o[1], o[C - 2], o[C - 1]));
+        } else {
+            dst[2 * lane] = (T)o[0];
+            dst[2 * lane + 1] = (T)o[1];
+        }
     }
 }
 

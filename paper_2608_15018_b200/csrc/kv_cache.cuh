@@ -33,22 +33,18 @@ __global__ void __launch_bounds__(128) kv_write_kernel(KvWriteArgs a)
     const int lane = threadIdx.x & 31;
     const int tok = blockIdx.x * 4 + (threadIdx.x >> 5);
     if (tok >= a.n_tokens) return;
-    int pos = -1, s = -1;
-    for (int s0 = 0; s0 < a.n_seq && s < 0; s0 += 32) {
-        const int i = s0 + lane;
-        int lo = 0, hi = 0;
-        if (i < a.n_seq) {
-            lo = __ldg(a.seq_start + i);
-            hi = __ldg(a.seq_start + i + 1);
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, tok >= lo && tok < hi);
-        if (hit) {
-            const int l = __ffs((int)hit) - 1;
-            s = s0 + l;
-            pos = tok - __shfl_sync(0xffffffffu, lo, l);
-        }
+    // the last sequence that begins at or before the token, 32 places at a time
+    int lo = 0, hi = a.n_seq;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, i = lo + lane * step;
+        const unsigned before = __ballot_sync(0xffffffffu, i < hi && __ldg(a.seq_start + i) <= tok);
+        if (!before) break;
+        lo += (31 - __clz((int)before)) * step;
+        hi = min(hi, lo + step);
     }
-    if (s < 0) return;
+    const int s = lo;
+    const long long pos = (long long)tok - __ldg(a.seq_start + s);
+    if (pos < 0 || tok >= __ldg(a.seq_start + s + 1)) return;
     const long long p = (long long)__ldg(a.first + s) + pos;
     if (p < 0 || p >= ((long long)a.table_width << a.c.page_shift)) return;
     const int page = __ldg(a.page_table + (long long)s * a.table_width + (p >> a.c.page_shift));

@@ -49,6 +49,22 @@ def test_write(dtype, page, heads, dim):
     assert same(cache, k, v)
 
 
+@pytest.mark.parametrize("n_seq", [31, 33, 1000, 40000])
+def test_write_of_many_sequences(n_seq):
+    """Many of them empty, some at the same offset."""
+    rng = random.Random(n_seq)
+    lengths = [rng.choice([0, 0, 1, 3]) for _ in range(n_seq)]
+    cache, k, v = pool(torch.bfloat16, 1, n_seq + 1, 1, 16, 64)
+    new = torch.randn((sum(lengths), 1, 64), device=DEV).bfloat16()
+    table = torch.randperm(n_seq, device=DEV).to(torch.int32).view(n_seq, 1).contiguous()
+    binding.kv_write(cache, 0, new, new, table, torch.full((n_seq,), 5, dtype=torch.int32, device=DEV), ints(offsets(lengths)))
+    owner = torch.repeat_interleave(torch.arange(n_seq, device=DEV), torch.tensor(lengths, device=DEV))
+    place = 5 + torch.arange(sum(lengths), device=DEV) - torch.tensor(offsets(lengths), device=DEV)[owner]
+    for x in (k, v):
+        x[0, table[owner, 0].long(), 0, place] = new[:, 0]
+    assert same(cache, k, v)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_write_leaves_out_what_has_no_place(dtype):
     cache, k, v = pool(dtype, 1, 6, 2, 16, 64)

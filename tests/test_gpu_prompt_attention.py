@@ -140,3 +140,23 @@ def test_scale_and_captured_call(dtype):
     g.replay()
     torch.cuda.synchronize()
     check(out, q, k, v, [10, 323], dtype, rng)
+
+
+@pytest.mark.parametrize("dtype,n", [(torch.bfloat16, 140000), (torch.float32, 20000)])
+def test_very_many_sequences(dtype, n):
+    """More items than a million: prompts of one token, whose output is their value."""
+    gen = torch.Generator(device=DEV).manual_seed(23)
+    q, k = (torch.randn((n, 8, 64), generator=gen, device=DEV).to(dtype) for _ in range(2))
+    v = torch.randn((n, 8, 64), generator=gen, device=DEV).to(dtype)
+    out = run(q, k, v, torch.arange(n + 1, dtype=torch.int32, device=DEV))
+    assert torch.equal(out, v)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim", [(16, 16, 128), (32, 8, 64)])
+def test_every_run_gives_the_same_bits(heads, kv_heads, dim):
+    lengths = [1500, 3, 700, 129, 2500, 64]
+    q, k, v, starts = inputs(29, torch.bfloat16, heads, kv_heads, dim, lengths)
+    want = run(q, k, v, starts)
+    outs = [binding.prompt_attention(q, k, v, starts) for _ in range(40)]
+    assert binding.attention_status() == 0
+    assert all(torch.equal(o, want) for o in outs)

@@ -229,3 +229,25 @@ def test_on_a_stream_of_its_own():
     junk = [torch.full((1 << 22,), float("nan"), device=DEV) for _ in range(4)]      # would land in a workspace given back early
     torch.cuda.synchronize()
     assert len(junk) == 4 and all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("heads,kv_heads,nodes,contexts", [
+    (16, 16, 16, [32000]), (8, 1, 8, [20000, 7]), (16, 16, 8, [8000] * 8), (32, 8, 64, [3000, 9000, 100]), (16, 4, 1, [700] * 40)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_every_run_gives_the_same_bits(heads, kv_heads, nodes, contexts, dim):
+    """Work is cut by lengths alone, so runs do not differ; a tile taken from another place than its own would show."""
+    rng = random.Random(97)
+    b = Batch(101, torch.bfloat16, heads, kv_heads, dim, 64, contexts, [random_tree(rng, nodes) for _ in contexts])
+    want = run(b)
+    b.check(want, rng, 30)
+    outs = [binding.tree_attention(b.q, b.cache, 0, b.page_table, b.context, b.seq_start, b.parent) for _ in range(40)]
+    assert binding.attention_status() == 0
+    assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_hundreds_of_sequences(dtype):
+    rng = random.Random(103)
+    contexts = [rng.choice([0, 3, 40, 130, 600]) for _ in range(333)]
+    b = Batch(107, dtype, 32, 8, 64, 32, contexts, [random_tree(rng, rng.choice([0, 1, 1, 2, 17])) for _ in contexts])
+    b.check(run(b), rng, 300)
