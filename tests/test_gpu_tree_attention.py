@@ -251,3 +251,12 @@ def test_hundreds_of_sequences(dtype):
     contexts = [rng.choice([0, 3, 40, 130, 600]) for _ in range(333)]
     b = Batch(107, dtype, 32, 8, 64, 32, contexts, [random_tree(rng, rng.choice([0, 1, 1, 2, 17])) for _ in contexts])
     b.check(run(b), rng, 300)
+
+
+def test_more_work_than_is_counted_is_refused():
+    """Refused by its sizes, before anything is read: 2^20 tokens over 2^28 positions."""
+    b = Batch(109, torch.bfloat16, 8, 4, 64, 16, [10], [[-1]])
+    p = b.q.data_ptr()
+    lib = binding.load_library()
+    rc = lib.s2moe_tree_attention(b.cache._ref, 0, 1, 1 << 20, 8, p, 512, p, 1 << 24, p, p, 1 << 20, None, None, 0.1, p, p, 1 << 40, None)
+    assert rc == binding.ERANGE
