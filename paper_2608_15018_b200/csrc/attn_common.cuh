@@ -119,8 +119,9 @@ __device__ __forceinline__ void attn_ancestors_all(const AttnArgs &a, const Attn
 template <bool PAGED>
 __device__ __forceinline__ int attn_limit(const AttnSeq &q, int t)
 {
-    const int lim = PAGED ? q.ctx + max(q.nodes - q.n + t, 0) + 1 : t + 1;
-    return min(lim, q.total);
+    if (!PAGED) return min(t + 1, q.total);
+    const int node = max(q.nodes - q.n + t, 0);
+    return node < q.total - q.ctx ? q.ctx + node + 1 : q.total;
 }
 
 // does a row see the key; lim from attn_limit, anc from attn_ancestors (all ones for chains)

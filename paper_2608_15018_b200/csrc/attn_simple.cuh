@@ -399,14 +399,24 @@ __global__ void __launch_bounds__(128) attn_join_kernel(AttnArgs a, int grid, in
         blocks = __shfl_sync(0xffffffffu, it.rts, l0);
         first = it.base + __shfl_sync(0xffffffffu, it.inc - it.my, l0);
     }
+    // where a head's row lies, and the CTAs of its pieces
+    int h = 0, r = 0, c0 = 0, c1 = 0;
+    bool second = false;                                       // the first piece is its CTA's second
+    auto locate = [&](int head) {
+        h = head / a.group;
+        const int row = t * a.group + head - h * a.group, rt = row / a.rows_tile, u0 = first + (h * blocks + rt) * tiles;
+        r = row - rt * a.rows_tile;
+        c0 = cut.owner(u0);
+        c1 = cut.owner(u0 + tiles - 1);
+        second = cut.start(c0) < u0;
+    };
+    if (hit) locate(head0);
     // (every thread waits: what follows in the stream starts when this kernel has ended, and the one in front must have too)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (!hit) return;
     for (int head = head0; head < head0 + each; ++head) {
-        const int h = head / a.group, row = t * a.group + head - h * a.group, rt = row / a.rows_tile, r = row - rt * a.rows_tile;
-        const int u0 = first + (h * blocks + rt) * tiles, c0 = cut.owner(u0), c1 = cut.owner(u0 + tiles - 1);
-        if (c0 == c1) continue;                                    // a whole item is written out already
-        const bool second = cut.start(c0) < u0;                    // the first piece is its CTA's second
+        if (head > head0) locate(head);
+        if (c0 == c1) continue;                                // a whole item is written out already
         float m = -CUDART_INF_F, l = 0.f, o[C];
 #pragma unroll
         for (int i = 0; i < C; ++i) o[i] = 0.f;

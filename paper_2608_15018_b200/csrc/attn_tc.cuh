@@ -38,6 +38,9 @@ constexpr int kAttnTile = 128;
 constexpr int kAttnThreads = 384;                 // 8 softmax warps, 2 for matrix instructions, 2 for copies
 constexpr int kAttnHalf = 128 * 128;              // bytes of 128 rows x 64 columns
 constexpr int kAttnPart = 3;                      // of 4 parts of a tile's weights, those handed over first
+// !PAIR: pieces with fewer tiles per group use the loop for all of them (32 sequences of 2000 positions: 134 us with the loop
+// alone, 126 so; one token over 700 positions 15.5 either way)
+constexpr int kAttnFew = 4;
 constexpr float kAttnSlack = 8.f;                 // log2 of the largest weight before the maximum is moved
 
 template <int D, bool PAIR>
@@ -539,7 +542,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     return see;
                 };
                 const float sc = a.scale_log2;
-                if (PAIR && !masked) {
+                if ((PAIR || n >= kAttnFew) && !masked) {
                     // the row in registers: one pass over S (a part's maximum is taken while the next part is on its way)
                     float s[4][32], mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
                     attn_ld32(s_at, s[0]);
@@ -574,10 +577,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                     sum[0] = attn_add2(sum[0], sum[1]);
                     l += sum[0].x + sum[0].y;
                 } else {
-                    // Two passes over S, 32 columns at a time in a loop: a quarter of the instructions, which is what
-                    // counts where a call has few tiles (the first pass through code costs more than running it), and
-                    // where the time is that of reading the cache.  Parts that no row of the warp sees (the upper triangle
-                    // of a prompt) are left out.
+                    // Two passes over S, 32 columns at a time in a loop: a quarter of the instructions, which is what counts
+                    // where a call has few tiles (the first pass through code costs more than running it).  Parts that no row
+                    // of the warp sees (the upper triangle of a prompt) are left out.
                     const int parts = min(4, max(0, (reach - key0 + 31) / 32));
                     auto part_of = [&](int j, float (&s)[32]) {
                         attn_ld32(s_at + 32 * j, s);

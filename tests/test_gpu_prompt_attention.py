@@ -43,7 +43,7 @@ def run(*args, **kw):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (16, 16, 128), (32, 8, 128), (9, 3, 64), (28, 4, 128), (64, 1, 64)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (16, 16, 128), (32, 8, 128), (9, 3, 64), (28, 4, 128), (64, 1, 64), (40, 1, 128)])
 def test_single_prompts(dtype, heads, kv_heads, dim):
     rng = random.Random(heads + dim)
     for n in (1, 2, 63, 64, 65, 127, 128, 129, 255, 256, 257, 500):

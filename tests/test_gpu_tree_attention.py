@@ -19,7 +19,7 @@ def run(b, **kw):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (16, 16, 128), (32, 8, 128), (9, 3, 64), (28, 4, 128), (64, 1, 64)])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (16, 16, 128), (32, 8, 128), (9, 3, 64), (28, 4, 128), (64, 1, 64), (40, 1, 128)])
 @pytest.mark.parametrize("page", [16, 128])
 def test_one_tree(dtype, heads, kv_heads, dim, page):
     rng = random.Random(heads * dim + page)
