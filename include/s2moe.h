@@ -445,8 +445,8 @@ typedef struct {
  *              sequence are left out and their rows of out stay as they are
  *   out        dev [n_tokens][n_heads][head_dim], 16-byte aligned, must not overlap the inputs
  * A key that a row does not see has no part in it, whatever it holds (infinities and NaN too).
- * Errors: EINVAL (null, alignment, heads, head_dim, scale negative or not finite), ERANGE (n_tokens * n_heads or
- * n_seq * n_kv_heads beyond 2^30), ECUDA.
+ * Errors: EINVAL (null, alignment, heads, head_dim, scale negative or not finite), ERANGE (n_seq beyond 2^20,
+ * n_tokens * n_heads or n_seq * n_kv_heads beyond 2^30), ECUDA.
  */
 int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32_t n_heads, int32_t n_kv_heads,
                            int32_t head_dim, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
@@ -474,7 +474,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
  *   workspace    dev, 16-byte aligned, at least what s2moe_tree_attention_workspace says; contents do not matter
  *                before or after.  Calls that may run at the same time need one each, captured graphs too.
  * One token per sequence is plain decoding.  Results depend on the arguments alone, not on timing.
- * Errors: EINVAL, ERANGE (layer; n_tokens * n_heads beyond 2^30, table_width * page_size beyond 2^31; more pieces of work than
+ * Errors: EINVAL, ERANGE (layer; n_seq beyond 2^20, n_tokens * n_heads beyond 2^30, table_width * page_size beyond 2^31; more pieces of work than
  * the kernels count in 32 bits: n_kv_heads * rows / 128 * positions / 128 of one sequence beyond 2^26), ECUDA.
  */
 int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_seq, int32_t n_tokens, int32_t n_heads,

@@ -26,6 +26,7 @@ namespace {
 __device__ int g_attn_status;
 
 constexpr int64_t kMaxRows = 1 << 30;      // rows (token, query head) of a call
+constexpr int kMaxSeqs = 1 << 20;          // sequences of a call: the kernels look through them 32 at a time
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 int elem_size(int dtype) { return dtype == S2MOE_F32 ? 4 : 2; }
@@ -273,7 +274,7 @@ int s2moe_prompt_attention(int32_t dtype, int32_t n_seq, int32_t n_tokens, int32
     if (q_stride % per16 || k_stride % per16 || v_stride % per16) return S2MOE_EINVAL;
     if (q_stride < (int64_t)n_heads * head_dim || k_stride < (int64_t)n_kv_heads * head_dim || v_stride < (int64_t)n_kv_heads * head_dim)
         return S2MOE_EINVAL;
-    if ((int64_t)n_tokens * n_heads > kMaxRows || (int64_t)n_seq * n_kv_heads > kMaxRows) return S2MOE_ERANGE;
+    if ((int64_t)n_tokens * n_heads > kMaxRows || n_seq > kMaxSeqs || (int64_t)n_seq * n_kv_heads > kMaxRows) return S2MOE_ERANGE;
     AttnArgs a{};
     a.q = q; a.k = k; a.v = v; a.out = out;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride;
@@ -320,7 +321,7 @@ int s2moe_tree_attention(const s2moe_kv_cache *cache, int32_t layer, int32_t n_s
     if (!q || !page_table || !context || !seq_start || !out) return S2MOE_EINVAL;
     if (!aligned16(q) || !aligned16(out) || q_stride % (16 / elem_size(cache->dtype)) || q_stride < (int64_t)n_heads * cache->head_dim)
         return S2MOE_EINVAL;
-    if ((int64_t)n_tokens * n_heads > kMaxRows || (int64_t)table_width * cache->page_size > INT32_MAX - 128) return S2MOE_ERANGE;
+    if ((int64_t)n_tokens * n_heads > kMaxRows || n_seq > kMaxSeqs || (int64_t)table_width * cache->page_size > INT32_MAX - 128) return S2MOE_ERANGE;
     const DeviceFacts *facts = device_facts();
     if (!facts) return S2MOE_ECUDA;
     const int n_sm = facts->n_sm;

@@ -36,7 +36,7 @@ def test_prompt_attention_refuses(change):
 
 
 def test_prompt_attention_sizes():
-    assert prompt(n_tokens=2 ** 29) == binding.ERANGE
+    assert prompt(n_tokens=2 ** 29) == binding.ERANGE and prompt(n_seq=2 ** 20 + 1) == binding.ERANGE
     assert prompt(n_tokens=0) == binding.OK and prompt(n_seq=0) == binding.OK
 
 
@@ -70,7 +70,7 @@ def test_tree_attention_sizes():
     assert tree(None) == binding.EINVAL
     assert tree(cache(), layer=2) == binding.ERANGE and tree(cache(), layer=-1) == binding.ERANGE
     assert tree(cache(), n_tokens=2 ** 29, n_nodes=2 ** 29) == binding.ERANGE
-    assert tree(cache(), table_width=2 ** 27) == binding.ERANGE
+    assert tree(cache(), table_width=2 ** 27) == binding.ERANGE and tree(cache(), n_seq=2 ** 20 + 1) == binding.ERANGE
     assert tree(cache(n_pages=2 ** 26)) == binding.ERANGE
     assert tree(cache(), n_tokens=0, n_nodes=0) == binding.OK and tree(cache(), n_seq=0) == binding.OK
     assert binding.load_library().s2moe_attention_status(None) == binding.EINVAL
